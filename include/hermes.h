@@ -398,14 +398,182 @@ int hermes_check_enable(hermes_ctx *ctx, int on);
  * launch of one kernel class while enabled.  Kernel ids: 0 append copy (done
  * inside the attention launch, whose time holds it: counted, with 0 ms),
  * 1 chunk attention, 2 attention-mass sweep, 3 score+select, 4 gather (and
- * re-indexing), 5 query attention, 6 summary reduction, 7 guidance scoring.  hermes_profile_read waits for the recorded events and
+ * re-indexing), 5 query attention, 6 summary reduction, 7 guidance scoring, 8 packing
+ * into pages.  hermes_profile_read waits for the recorded events and
  * returns the summed milliseconds and the launch count since the last read.
  */
 enum { HERMES_K_APPEND = 0, HERMES_K_ATTN = 1, HERMES_K_COLSUM = 2, HERMES_K_SELECT = 3,
        HERMES_K_GATHER = 4, HERMES_K_QUERY = 5, HERMES_K_SUMMARY = 6, HERMES_K_GUIDE = 7,
-       HERMES_K_COUNT = 8 };
+       HERMES_K_PACK = 8, HERMES_K_COUNT = 9 };
 int hermes_profile_enable(hermes_ctx *ctx, int on);
 int hermes_profile_read(hermes_ctx *ctx, int kernel_id, double *ms_total, int64_t *count);
+
+/*
+ * Pages: K and V of many sequences in one pool of pages of page_rows tokens, in
+ * bf16 or in 4 bits, for text that is answered from the compact memory: a
+ * context's caches are packed into pages (hermes_page_pack), new rows are rotated
+ * and appended to the pages of their sequence (hermes_page_append), and attend
+ * over them (hermes_page_attend), many rows a sequence for a prompt or one for a
+ * generated token.  A sequence is a stream, or one layer of it: pages of one pool
+ * may serve several layers, each with its own table and length.
+ *
+ * These calls keep no state: the pool, the tables and the lengths are the
+ * caller's, on the device, so that a captured call can be replayed with tables
+ * and lengths that have changed.  They allocate nothing, never synchronise, and
+ * run on `stream` of the current device.  Two calls may run at once if neither
+ * writes what the other uses: rows that hermes_page_append stores must be on the
+ * device before a call on another stream reads them, and calls at once need a
+ * workspace each.
+ *
+ * The layout of a page.  A page holds, for each KV head in turn, a block of four
+ * parts (R = page_rows, d = head_dim, s = d / 16 channels a piece):
+ *      K  [R][d]                    rows of channels
+ *      V  [R / 4][16][4][s]         of every four rows, piece by piece
+ *      K scales  [R][d / 32]        FP4 only: one byte for 32 channels
+ *      V scales  [R / 4][d / 32][4]
+ * FP4 (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) keeps two channels a
+ * byte, the even one in the low half; a scale byte b stands for 2^(b - 127).
+ * The 32 values of a block are stored with the least power of two 2^e of which
+ * 7 x 2^e covers their largest magnitude (so that no value is off by more than
+ * half of the widest step, the one from 4 to 6), e clamped to -119 .. 125; each
+ * value goes to the nearest code, a tie to the even one, and beyond 6 to 6.  Codes
+ * times scales are exact in bf16.  A block with an infinity or a NaN reads back as
+ * NaN (byte 255).
+ */
+enum { HERMES_PAGE_BF16 = 0, HERMES_PAGE_FP4 = 1 };
+
+/* Bits that a call ORs into the pool's status word when it meets tables, lengths
+ * or row starts on the device that do not fit the pool or the batch. */
+enum {
+  HERMES_PAGE_BAD_ID = 1,      /* a page id outside 0 .. n_pages - 1: its rows are not
+                                  stored, and read as zeros                           */
+  HERMES_PAGE_BAD_LENGTH = 2,  /* a length below 0 or beyond the sequence's table: the
+                                  sequence counts as empty                            */
+  HERMES_PAGE_BAD_ROWS = 4     /* row starts that fall, or leave 0 .. n_rows: clamped  */
+};
+
+/*
+ *  format       HERMES_PAGE_*.
+ *  page_rows    tokens of a page: 16, 32, 64, 128 or 256.
+ *  n_pages      pages of the pool.
+ *  pages        device memory of n_pages x hermes_page_bytes, 16-byte aligned; needs
+ *               no initial values.
+ *  status       device int32 the HERMES_PAGE_BAD_* bits are ORed into, or NULL.
+ *               Nothing is read or written out of bounds, with or without it.
+ *  n_q_heads, n_kv_heads, head_dim, sm_scale, rope_theta, rope_axes,
+ *  mrope_section   as in hermes_config.
+ */
+typedef struct {
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t format;
+  int32_t page_rows;
+  int32_t n_pages;
+  void *pages;
+  int32_t *status;
+  double sm_scale;
+  double rope_theta;
+  int32_t rope_axes;
+  int32_t mrope_section[3];
+} hermes_page_pool;
+
+/*
+ * The sequences of one call, and their rows in its stacked inputs.  Rows
+ * row_start[b] .. row_start[b + 1] - 1 belong to sequence b and are its last
+ * tokens: with n of them, row i is token kv_len[b] - n + i.  Token t lives in row
+ * t % page_rows of page tables[b][t / page_rows].
+ *  n_seqs       sequences (0 is allowed: the call does nothing).
+ *  n_rows       rows of the stacked inputs; rows that belong to no sequence
+ *               (before row_start[0], from row_start[n_seqs] on) are neither read nor
+ *               written.
+ *  max_rows     most rows of a sequence, and max_len the greatest length (0: n_rows,
+ *               and what the tables hold).  They only choose how the work is cut:
+ *               longer sequences are handled all the same, slower.
+ *  max_pages    entries of a table; those past a sequence's last token are not read.
+ *  row_start    device int32 [n_seqs + 1], not falling; NULL: one row a sequence
+ *               (n_rows = n_seqs).
+ *  kv_len       device int32 [n_seqs]: lengths, the call's own rows among them.
+ *  tables       device int32 [n_seqs][max_pages]: page ids.  Sequences may share
+ *               pages that no call writes; of rows that are stored twice in one call,
+ *               either may stay.
+ */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_rows;
+  int32_t max_rows;
+  int32_t max_len;
+  int32_t max_pages;
+  const int32_t *row_start;
+  const int32_t *kv_len;
+  const int32_t *tables;
+} hermes_page_batch;
+
+/* Bytes of one page (0 on a bad pool; pages and status are not looked at). */
+size_t hermes_page_bytes(const hermes_page_pool *pool);
+
+/*
+ * Append rows: rotate every row's query and key to its position (rotate-half
+ * pairs, angles and rotation in fp64, rounded to fp32 and then to bf16, as
+ * hermes_compress rotates), store the key and the value in the row's page, and
+ * write the rotated query to q_out.
+ *  q            device bf16, rows of n_q_heads x head_dim, q_stride elements apart;
+ *               NULL (and q_out NULL): no queries.
+ *  k, v         device bf16, rows of n_kv_heads x head_dim, k_stride and v_stride
+ *               elements apart (the strides are multiples of 8; q, k and v may be parts
+ *               of one buffer, the output of a fused projection).
+ *  rope         device int32 [n_rows] positions; with rope_axes 3 [3][n_rows] t, h
+ *               and w coordinates.  NULL: k is rotated already (q must be NULL).
+ *  q_out        device bf16 [n_rows][n_q_heads][head_dim]; may be q where q has that
+ *               layout.
+ * A row whose token would lie before the sequence's first (more rows than the length) is
+ * rotated, and not stored.  Positions need not be those of the sequence.
+ * Errors: EINVAL (null, misaligned or inconsistent arguments, a size out of
+ * range), ENOTSUP (head_dim), EHIP.
+ */
+int hermes_page_append(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,
+                       int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                       const int32_t *rope, void *q_out, void *stream);
+
+/* Bytes of workspace that hermes_page_attend needs for calls of `batch` (its
+ * device pointers are not looked at; 0 if none, or on bad arguments). */
+size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_page_batch *batch);
+
+/*
+ * Causal attention of every sequence's rows over its pages: row i of n sees the
+ * tokens 0 .. kv_len - n + i (its own among them, so they are appended first).
+ *  q            device bf16, rows of n_q_heads x head_dim, q_stride elements apart.
+ *  out          device bf16 [n_rows][n_q_heads][head_dim].
+ *  lse          device fp32 [n_rows][n_q_heads] or NULL: ln sum exp of the scaled
+ *               scores (joins the result with that over other keys).
+ *  workspace    device memory of hermes_page_workspace_bytes, 16-byte aligned (may be
+ *               NULL if that is 0); free again when the call's work is done.
+ * A row that sees no token gets zeros, and -infinity in lse.  Stored values are
+ * taken to be finite, as q is.
+ * Errors: EINVAL, ENOTSUP, ECAPACITY (workspace too small), EHIP.
+ */
+int hermes_page_attend(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,
+                       int64_t q_stride, void *out, float *lse, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Read rows back: the stored key and value of every row of the batch, as device
+ * bf16 [n_rows][n_kv_heads][head_dim] (either may be NULL).  A row before the
+ * sequence's first token gets zeros.
+ * Errors: EINVAL, ENOTSUP, EHIP.
+ */
+int hermes_page_read(const hermes_page_pool *pool, const hermes_page_batch *batch, void *k, void *v, void *stream);
+
+/*
+ * Pack the current cache of one layer, or of all, into pages (its keys as they
+ * are, rotated): rows 0 .. len - 1 go to the pages of tables, device int32
+ * [max_pages], or [n_layers][max_pages] with HERMES_ALL_LAYERS, and the length to
+ * kv_len, device int32 [1] or [n_layers].  The context is not changed, and the
+ * pages need it no longer.  Not allowed between an append and its compress.
+ * Errors: EINVAL (also a pool of another n_kv_heads or head_dim), ECAPACITY (a
+ * layer longer than its table), ENOTSUP, ESTATE, EHIP (poisons the context).
+ */
+int hermes_page_pack(hermes_ctx *ctx, int32_t layer, const hermes_page_pool *pool, const int32_t *tables,
+                     int32_t max_pages, int32_t *kv_len, void *stream);
 
 #ifdef __cplusplus
 }

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "hermes_internal.h"
+#include "pages_internal.h"
 
 using namespace hermes;
 
@@ -1357,6 +1358,36 @@ int hermes_check_enable(hermes_ctx *ctx, int on) {
   if (ctx == nullptr) return HERMES_EINVAL;
   ctx->check = on != 0;
   return HERMES_OK;
+}
+
+int hermes_page_pack(hermes_ctx *ctx, int32_t layer, const hermes_page_pool *pool, const int32_t *tables,
+                     int32_t max_pages, int32_t *kv_len, void *stream) {
+  if (ctx == nullptr) return HERMES_EINVAL;
+  if (ctx->poisoned) return HERMES_ESTATE;
+  const int rc = check_page_memory(pool);
+  if (rc != HERMES_OK) return rc;
+  const int L = ctx->L;
+  if (layer != HERMES_ALL_LAYERS && (layer < 0 || layer >= L)) return HERMES_EINVAL;
+  if (pool->n_kv_heads != ctx->Hkv || pool->head_dim != ctx->D) return HERMES_EINVAL;
+  if (tables == nullptr || kv_len == nullptr || !aligned(tables, 4) || !aligned(kv_len, 4) || max_pages < 1)
+    return HERMES_EINVAL;
+  if (ctx->n_appended != 0) return HERMES_ESTATE;
+  PagePackArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.pool = page_pool_of(pool);
+  a.tables = tables;
+  a.kv_len = kv_len;
+  a.max_pages = max_pages;
+  for (int l = 0; l < L; ++l) {
+    if (layer != HERMES_ALL_LAYERS && l != layer) continue;
+    if (ctx->len[l] > (int64_t)max_pages * pool->page_rows) return HERMES_ECAPACITY;
+    a.k[a.n_list] = static_cast<const uint16_t *>(ctx->bufs[l].k[ctx->cur[l]]);
+    a.v[a.n_list] = static_cast<const uint16_t *>(ctx->bufs[l].v[ctx->cur[l]]);
+    a.len[a.n_list] = ctx->len[l];
+    ++a.n_list;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return ctx->run(HERMES_K_PACK, s, [&] { return launch_page_pack(a, ctx->D, pool->format, s); });
 }
 
 int hermes_profile_enable(hermes_ctx *ctx, int on) {

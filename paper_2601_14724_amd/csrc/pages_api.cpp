@@ -1,0 +1,228 @@
+// Host side of the pages: argument checks, the cut of an attention call, and the
+// launches on the caller's stream.  Nothing here keeps state or allocates.
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+
+#include "pages_internal.h"
+
+using namespace hermes;
+
+namespace hermes {
+
+namespace {
+
+constexpr double kLog2e = 1.4426950408889634;
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+int64_t block_bytes(const hermes_page_pool *p) {
+  const int64_t d = p->head_dim, row = p->format == HERMES_PAGE_FP4 ? d / 2 + d / 32 : 2 * d;
+  return 2 * row * p->page_rows;
+}
+
+int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
+  if (b == nullptr || b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_len < 0) return HERMES_EINVAL;
+  if (b->n_rows > 1 << 30 || (b->row_start == nullptr && b->n_rows != b->n_seqs)) return HERMES_EINVAL;
+  if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
+  if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
+  if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;
+  return HERMES_OK;
+}
+
+int check_batch_memory(const hermes_page_batch *b) {
+  if (b->kv_len == nullptr || b->tables == nullptr) return HERMES_EINVAL;
+  if (!aligned(b->row_start, 4) || !aligned(b->kv_len, 4) || !aligned(b->tables, 4)) return HERMES_EINVAL;
+  return HERMES_OK;
+}
+
+// rows of bf16 `width` wide, `stride` apart
+bool good_rows(const void *p, int64_t stride, int64_t width) {
+  return p != nullptr && aligned(p, 16) && stride >= width && stride % 8 == 0;
+}
+
+PageSeqs seqs_of(const hermes_page_batch *b) {
+  return PageSeqs{b->row_start, b->kv_len, b->tables, b->n_seqs, b->n_rows, b->max_pages};
+}
+
+int64_t over(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+// The cut of an attention call, from what the host knows of it.
+PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
+  const int64_t G = p->n_q_heads / p->n_kv_heads;
+  const int64_t max_rows = b->max_rows > 0 && b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
+  const int64_t table = (int64_t)b->max_pages * p->page_rows;
+  const int64_t max_len = b->max_len > 0 && b->max_len < table ? b->max_len : table;
+  const int64_t P = max_rows * G;
+  PagePlan x;
+  x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 64;
+  const int64_t tiles = over(P, x.rows);
+  x.tiles = (int32_t)(tiles < 65535 ? tiles : 65535);
+  // two workgroups a CU, each of at least a step (of 32 keys) for its four waves
+  const int64_t pairs = (int64_t)b->n_seqs * p->n_kv_heads * x.tiles;
+  int64_t splits = 2 * kStreamSlots / pairs;
+  if (splits > over(max_len, 128)) splits = over(max_len, 128);
+  if (splits < 1) splits = 1;
+  x.range = (int32_t)(over(over(max_len, splits), 128) * 128);
+  x.splits = (int32_t)over(max_len, x.range);
+  return x;
+}
+
+size_t workspace_of(const hermes_page_pool *p, const hermes_page_batch *b, const PagePlan &x) {
+  if (x.splits == 1) return 0;
+  return sizeof(float) * (size_t)x.splits * (size_t)b->n_rows * p->n_q_heads * (p->head_dim + 2);
+}
+
+void fill_rope(const hermes_page_pool *p, PageAppendArgs *a) {
+  const double base = p->rope_theta > 0.0 ? p->rope_theta : 1.0e6;
+  const int half = p->head_dim / 2;
+  for (int j = 0; j < half; ++j) a->inv_freq[j] = std::pow(base, (-2.0 * (double)j) / (double)p->head_dim);
+  a->axes = p->rope_axes == 3 ? 3 : 1;
+  const int *sec = p->mrope_section;
+  if (sec[0] == 0 && sec[1] == 0 && sec[2] == 0) {
+    a->section[0] = half / 4;
+    a->section[1] = (half - half / 4) / 2;
+    a->section[2] = half - a->section[0] - a->section[1];
+  } else {
+    for (int i = 0; i < 3; ++i) a->section[i] = sec[i];
+  }
+}
+
+}  // namespace
+
+int check_page_pool(const hermes_page_pool *p) {
+  if (p == nullptr) return HERMES_EINVAL;
+  if (p->n_kv_heads < 1 || p->n_q_heads < p->n_kv_heads || p->n_q_heads % p->n_kv_heads != 0) return HERMES_EINVAL;
+  if (p->n_q_heads > 1 << 16) return HERMES_EINVAL;
+  if (p->head_dim != 64 && p->head_dim != 128) return HERMES_ENOTSUP;
+  if (p->format != HERMES_PAGE_BF16 && p->format != HERMES_PAGE_FP4) return HERMES_EINVAL;
+  if (p->page_rows < 16 || p->page_rows > 256 || (p->page_rows & (p->page_rows - 1)) != 0) return HERMES_EINVAL;
+  if (p->n_pages < 1) return HERMES_EINVAL;
+  if (!std::isfinite(p->sm_scale) || !std::isfinite(p->rope_theta)) return HERMES_EINVAL;
+  if (p->rope_axes != 0 && p->rope_axes != 1 && p->rope_axes != 3) return HERMES_EINVAL;
+  if (p->rope_axes == 3) {
+    const int *sec = p->mrope_section;
+    if (sec[0] < 0 || sec[1] < 0 || sec[2] < 0) return HERMES_EINVAL;
+    const int64_t sum = (int64_t)sec[0] + sec[1] + sec[2];
+    if (sum != 0 && sum != p->head_dim / 2) return HERMES_EINVAL;
+  }
+  return HERMES_OK;
+}
+
+int check_page_memory(const hermes_page_pool *p) {
+  const int rc = check_page_pool(p);
+  if (rc != HERMES_OK) return rc;
+  if (p->pages == nullptr || !aligned(p->pages, 16) || !aligned(p->status, 4)) return HERMES_EINVAL;
+  return HERMES_OK;
+}
+
+PagePool page_pool_of(const hermes_page_pool *p) {
+  PagePool x;
+  x.pages = static_cast<uint8_t *>(p->pages);
+  x.status = p->status;
+  x.block_bytes = (int32_t)block_bytes(p);
+  x.page_bytes = block_bytes(p) * p->n_kv_heads;
+  x.log_rows = 0;
+  while ((1 << x.log_rows) < p->page_rows) ++x.log_rows;
+  x.n_pages = p->n_pages;
+  x.Hq = p->n_q_heads;
+  x.Hkv = p->n_kv_heads;
+  return x;
+}
+
+}  // namespace hermes
+
+extern "C" {
+
+size_t hermes_page_bytes(const hermes_page_pool *pool) {
+  if (check_page_pool(pool) != HERMES_OK) return 0;
+  return (size_t)(block_bytes(pool) * pool->n_kv_heads);
+}
+
+size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_page_batch *batch) {
+  if (check_page_pool(pool) != HERMES_OK || check_batch(pool, batch) != HERMES_OK) return 0;
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return 0;
+  return workspace_of(pool, batch, plan_of(pool, batch));
+}
+
+int hermes_page_append(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,
+                       int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                       const int32_t *rope, void *q_out, void *stream) {
+  int rc = check_page_memory(pool);
+  if (rc == HERMES_OK) rc = check_batch(pool, batch);
+  if (rc != HERMES_OK) return rc;
+  if ((q == nullptr) != (q_out == nullptr) || (q != nullptr && rope == nullptr)) return HERMES_EINVAL;
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return HERMES_OK;
+  if ((rc = check_batch_memory(batch)) != HERMES_OK) return rc;
+  const int64_t qw = (int64_t)pool->n_q_heads * pool->head_dim, kw = (int64_t)pool->n_kv_heads * pool->head_dim;
+  if (!good_rows(k, k_stride, kw) || !good_rows(v, v_stride, kw) || !aligned(rope, 4)) return HERMES_EINVAL;
+  if (q != nullptr) {
+    if (!good_rows(q, q_stride, qw) || !aligned(q_out, 16)) return HERMES_EINVAL;
+    if (q == q_out && q_stride != qw) return HERMES_EINVAL;
+  }
+  PageAppendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.pool = page_pool_of(pool);
+  a.seqs = seqs_of(batch);
+  a.q = static_cast<const uint16_t *>(q);
+  a.k = static_cast<const uint16_t *>(k);
+  a.v = static_cast<const uint16_t *>(v);
+  a.q_out = static_cast<uint16_t *>(q_out);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.rope = rope;
+  if (rope != nullptr) fill_rope(pool, &a);
+  return launch_page_append(a, pool->head_dim, pool->format, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? HERMES_OK : HERMES_EHIP;
+}
+
+int hermes_page_attend(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,
+                       int64_t q_stride, void *out, float *lse, void *workspace, size_t ws_bytes, void *stream) {
+  int rc = check_page_memory(pool);
+  if (rc == HERMES_OK) rc = check_batch(pool, batch);
+  if (rc != HERMES_OK) return rc;
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return HERMES_OK;
+  if ((rc = check_batch_memory(batch)) != HERMES_OK) return rc;
+  const int64_t qw = (int64_t)pool->n_q_heads * pool->head_dim;
+  if (!good_rows(q, q_stride, qw) || out == nullptr || !aligned(out, 16) || !aligned(lse, 4)) return HERMES_EINVAL;
+  PageAttnArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.plan = plan_of(pool, batch);
+  const size_t need = workspace_of(pool, batch, a.plan);
+  if (need > 0) {
+    if (workspace == nullptr || !aligned(workspace, 16)) return HERMES_EINVAL;
+    if (ws_bytes < need) return HERMES_ECAPACITY;
+    a.opart = static_cast<float *>(workspace);
+    a.mlpart = a.opart + (size_t)a.plan.splits * batch->n_rows * pool->n_q_heads * pool->head_dim;
+  }
+  a.pool = page_pool_of(pool);
+  a.seqs = seqs_of(batch);
+  a.q = static_cast<const uint16_t *>(q);
+  a.q_stride = q_stride;
+  a.out = static_cast<uint16_t *>(out);
+  a.lse = lse;
+  const double scale = pool->sm_scale > 0.0 ? pool->sm_scale : 1.0 / std::sqrt((double)pool->head_dim);
+  a.scale_log2 = (float)(scale * kLog2e);
+  return launch_page_attend(a, pool->head_dim, pool->format, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? HERMES_OK : HERMES_EHIP;
+}
+
+int hermes_page_read(const hermes_page_pool *pool, const hermes_page_batch *batch, void *k, void *v, void *stream) {
+  int rc = check_page_memory(pool);
+  if (rc == HERMES_OK) rc = check_batch(pool, batch);
+  if (rc != HERMES_OK) return rc;
+  if (!aligned(k, 16) || !aligned(v, 16)) return HERMES_EINVAL;
+  if (batch->n_seqs == 0 || batch->n_rows == 0 || (k == nullptr && v == nullptr)) return HERMES_OK;
+  if ((rc = check_batch_memory(batch)) != HERMES_OK) return rc;
+  PageReadArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.pool = page_pool_of(pool);
+  a.seqs = seqs_of(batch);
+  a.k = static_cast<uint16_t *>(k);
+  a.v = static_cast<uint16_t *>(v);
+  return launch_page_read(a, pool->head_dim, pool->format, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? HERMES_OK : HERMES_EHIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,128 @@
+// Declarations shared by the host entry points of the pages (pages_api.cpp,
+// hermes_api.cpp) and their kernels (pages.hip, page_attention.hip).
+#pragma once
+
+#include "hermes_internal.h"
+
+namespace hermes {
+
+// A pool as the kernels see it.
+struct PagePool {
+  uint8_t *pages;
+  int32_t *status;          // or null
+  int64_t page_bytes;
+  int32_t block_bytes;      // of one KV head's block in a page
+  int32_t log_rows;         // page_rows = 1 << log_rows
+  int32_t n_pages;
+  int32_t Hq, Hkv;
+};
+
+// A call's sequences, as in hermes_page_batch.
+struct PageSeqs {
+  const int32_t *row_start, *kv_len, *tables;
+  int32_t n_seqs, n_rows, max_pages;
+};
+
+struct PageAppendArgs {
+  PagePool pool;
+  PageSeqs seqs;
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t *rope;      // [axes][n_rows], or null: k as it is
+  int32_t axes;
+  int32_t section[3];       // axes 3: frequency pairs of the t, h, w sections
+  double inv_freq[kMaxHalfDim];
+};
+
+struct PageReadArgs {
+  PagePool pool;
+  PageSeqs seqs;
+  uint16_t *k, *v;          // [n_rows][Hkv][d], either may be null
+};
+
+struct PagePackArgs {
+  PagePool pool;
+  const int32_t *tables;    // [n_list][max_pages]
+  int32_t *kv_len;          // [n_list]
+  int32_t max_pages, n_list;
+  const uint16_t *k[kMaxLayers], *v[kMaxLayers];
+  int32_t len[kMaxLayers];
+};
+
+// How an attention call is cut: tiles of `rows` packed rows (row, query head of
+// the KV head), and `splits` ranges of `range` keys each (the last one up to the
+// end, however long).
+struct PagePlan {
+  int32_t rows, splits, range, tiles;
+};
+
+struct PageAttnArgs {
+  PagePool pool;
+  PageSeqs seqs;
+  const uint16_t *q;
+  int64_t q_stride;
+  uint16_t *out;            // [n_rows][Hq][d]
+  float *lse;               // [n_rows][Hq] or null
+  float scale_log2;         // sm_scale * log2(e)
+  PagePlan plan;
+  float *opart;             // splits > 1: [splits][n_rows * Hq][d] unnormalised O
+  float *mlpart;            // [splits][n_rows * Hq][2] (max, sum), log2 domain
+};
+
+hipError_t launch_page_append(const PageAppendArgs &a, int head_dim, int format, hipStream_t s);
+hipError_t launch_page_read(const PageReadArgs &a, int head_dim, int format, hipStream_t s);
+hipError_t launch_page_pack(const PagePackArgs &a, int head_dim, int format, hipStream_t s);
+hipError_t launch_page_attend(const PageAttnArgs &a, int head_dim, int format, hipStream_t s);
+
+// Host checks of a pool and a batch (HERMES_OK or an error), and the kernels'
+// view of them.  check_page_memory also looks at the pool's pointers.
+int check_page_pool(const hermes_page_pool *p);
+int check_page_memory(const hermes_page_pool *p);
+PagePool page_pool_of(const hermes_page_pool *p);
+
+#ifdef __HIP__
+// Sequence b of a batch: its first stacked row, its rows and its length, with
+// whatever does not fit clamped and noted in the pool's status word.
+struct PageSeq {
+  int r0, n, len;
+};
+__device__ __forceinline__ void page_note(const PagePool &p, int bit) {
+  if (p.status != nullptr) atomicOr(p.status, bit);
+}
+__device__ __forceinline__ PageSeq page_seq(const PagePool &p, const PageSeqs &s, int b) {
+  PageSeq x;
+  if (s.row_start != nullptr) {
+    const int a0 = s.row_start[b], a1 = s.row_start[b + 1];
+    x.r0 = min(max(a0, 0), s.n_rows);
+    const int r1 = min(max(a1, x.r0), s.n_rows);
+    x.n = r1 - x.r0;
+    if (x.r0 != a0 || r1 != a1) page_note(p, HERMES_PAGE_BAD_ROWS);
+  } else {
+    x.r0 = b;
+    x.n = 1;
+  }
+  x.len = s.kv_len[b];
+  if (x.len < 0 || x.len > (int64_t)s.max_pages << p.log_rows) {
+    x.len = 0;
+    page_note(p, HERMES_PAGE_BAD_LENGTH);
+  }
+  return x;
+}
+// Byte offsets inside a KV head's block (see hermes.h): K row r, V rows 4 r4 ..
+// 4 r4 + 3, and their scales.
+template <int D, bool FP4>
+struct PageBlock {
+  static constexpr int kRow = FP4 ? D / 2 : 2 * D;          // bytes of a row of K (or of V)
+  static constexpr int kPiece = kRow / 16;                  // of a piece of V
+  static constexpr int kScales = D / 32;                    // of a row's scales
+  __device__ static __forceinline__ int k(int r) { return r * kRow; }
+  __device__ static __forceinline__ int v(int rows, int r4) { return rows * kRow + r4 * 4 * kRow; }
+  __device__ static __forceinline__ int ks(int rows, int r) { return 2 * rows * kRow + r * kScales; }
+  __device__ static __forceinline__ int vs(int rows, int r4) {
+    return 2 * rows * kRow + rows * kScales + r4 * 4 * kScales;
+  }
+};
+#endif
+
+}  // namespace hermes

@@ -24,10 +24,12 @@ OK, EINVAL, ECAPACITY, ESTATE, EHIP, ENOTSUP = 0, -1, -2, -3, -4, -5
 SHALLOW, MIDDLE, DEEP = 0, 1, 2
 ALL_LAYERS = -1
 MAX_LAYERS = 64
-K_APPEND, K_ATTN, K_COLSUM, K_SELECT, K_GATHER, K_QUERY, K_SUMMARY, K_GUIDE = range(8)
-KERNEL_NAMES = ("append", "attention", "colsum", "select", "gather", "query", "summary", "guide")
+K_APPEND, K_ATTN, K_COLSUM, K_SELECT, K_GATHER, K_QUERY, K_SUMMARY, K_GUIDE, K_PACK = range(9)
+KERNEL_NAMES = ("append", "attention", "colsum", "select", "gather", "query", "summary", "guide", "pack")
 REINDEX_NONE, REINDEX_EAGER, REINDEX_LAZY = 0, 1, 2
 SCORE_CHUNK, SCORE_GUIDANCE = 0, 1
+PAGE_BF16, PAGE_FP4 = 0, 1
+PAGE_BAD_ID, PAGE_BAD_LENGTH, PAGE_BAD_ROWS = 1, 2, 4
 
 EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_append_chunk_at", "hermes_guidance_score", "hermes_compress",
@@ -35,7 +37,9 @@ EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_kv_view", "hermes_kv_view_rope", "hermes_kv_view_mrope",
             "hermes_budget_from_weights", "hermes_kv_destroy", "hermes_strerror",
             "hermes_select_topk", "hermes_profile_enable", "hermes_profile_read",
-            "hermes_check_enable", "hermes_kv_init_static")
+            "hermes_check_enable", "hermes_kv_init_static",
+            "hermes_page_bytes", "hermes_page_workspace_bytes", "hermes_page_append",
+            "hermes_page_attend", "hermes_page_read", "hermes_page_pack")
 STATIC_WORKSPACE_BYTES = 128 << 20
 
 
@@ -64,6 +68,20 @@ class LayerBuffers(ctypes.Structure):
                 ("cap", ctypes.c_int32), ("init_len", ctypes.c_int32),
                 ("rpos", ctypes.c_void_p * 2), ("rpos_h", ctypes.c_void_p * 2),
                 ("rpos_w", ctypes.c_void_p * 2)]
+
+
+class PagePoolStruct(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("pages", ctypes.c_void_p), ("status", ctypes.c_void_p), ("sm_scale", ctypes.c_double),
+                ("rope_theta", ctypes.c_double), ("rope_axes", ctypes.c_int32),
+                ("mrope_section", ctypes.c_int32 * 3)]
+
+
+class PageBatchStruct(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("row_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p)]
 
 
 _vp, _i32, _i64, _dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
@@ -111,6 +129,19 @@ lib.hermes_profile_enable.restype = ctypes.c_int
 lib.hermes_profile_enable.argtypes = [_vp, ctypes.c_int]
 lib.hermes_profile_read.restype = ctypes.c_int
 lib.hermes_profile_read.argtypes = [_vp, ctypes.c_int, ctypes.POINTER(_dbl), ctypes.POINTER(_i64)]
+_pool_p, _batch_p = ctypes.POINTER(PagePoolStruct), ctypes.POINTER(PageBatchStruct)
+lib.hermes_page_bytes.restype = ctypes.c_size_t
+lib.hermes_page_bytes.argtypes = [_pool_p]
+lib.hermes_page_workspace_bytes.restype = ctypes.c_size_t
+lib.hermes_page_workspace_bytes.argtypes = [_pool_p, _batch_p]
+lib.hermes_page_append.restype = ctypes.c_int
+lib.hermes_page_append.argtypes = [_pool_p, _batch_p, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp]
+lib.hermes_page_attend.restype = ctypes.c_int
+lib.hermes_page_attend.argtypes = [_pool_p, _batch_p, _vp, _i64, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+lib.hermes_page_read.restype = ctypes.c_int
+lib.hermes_page_read.argtypes = [_pool_p, _batch_p, _vp, _vp, _vp]
+lib.hermes_page_pack.restype = ctypes.c_int
+lib.hermes_page_pack.argtypes = [_vp, _i32, _pool_p, _vp, _i32, _vp, _vp]
 
 
 class HermesError(RuntimeError):
@@ -351,6 +382,16 @@ class HermesKV:
                                       n, out.data_ptr(), _stream()), "hermes_query_attend")
         return out
 
+    def pack(self, pages: "KVPages", tables: torch.Tensor, kv_len: torch.Tensor, layer: int = ALL_LAYERS) -> None:
+        """Packs the current cache of one layer, or of all, into the pages of `tables`
+        (int32 [max_pages], or [L][max_pages]), and its length into kv_len (int32 [1] or [L])."""
+        lead = () if layer != ALL_LAYERS else (self.L,)
+        _need(tables, torch.int32, lead + (tables.shape[-1],), "tables")
+        _need(kv_len, torch.int32, lead or (1,), "kv_len")
+        with pages._here(tables, kv_len, self.k[0][0]):
+            check(lib.hermes_page_pack(self.ctx, layer, ctypes.byref(pages._pool), tables.data_ptr(), tables.shape[-1],
+                                       kv_len.data_ptr(), _stream()), "hermes_page_pack")
+
     def rewind(self) -> None:
         check(lib.hermes_kv_rewind(self.ctx), "hermes_kv_rewind")
 
@@ -414,6 +455,137 @@ class HermesKV:
             self.close()
         except Exception:
             pass
+
+
+class PageBatch:
+    """The sequences of a call on pages and their rows in its stacked inputs
+    (hermes_page_batch): page ids `tables` int32 [n_seqs][max_pages], lengths `kv_len`
+    int32 [n_seqs] with the call's own rows, and `row_start` int32 [n_seqs + 1] with
+    `n_rows` stacked rows (None: one row a sequence).  The tensors are read by every
+    call, and may change between calls.  `max_rows` and `max_len` (None: not known)
+    only choose how the work is cut."""
+
+    def __init__(self, tables: torch.Tensor, kv_len: torch.Tensor, row_start: Optional[torch.Tensor] = None,
+                 n_rows: Optional[int] = None, max_rows: Optional[int] = None, max_len: Optional[int] = None):
+        n = int(kv_len.shape[0])
+        _need(kv_len, torch.int32, (n,), "kv_len")
+        _need(tables, torch.int32, (n, tables.shape[-1]), "tables")
+        if row_start is not None:
+            _need(row_start, torch.int32, (n + 1,), "row_start")
+            if n_rows is None:
+                raise ValueError("n_rows: needed with row_start")
+        elif n_rows not in (None, n):
+            raise ValueError("n_rows: one row a sequence without row_start")
+        self.tables, self.kv_len, self.row_start = tables, kv_len, row_start
+        self.n_seqs, self.n_rows = n, n if n_rows is None else int(n_rows)
+        b = PageBatchStruct()
+        b.n_seqs, b.n_rows, b.max_pages = n, self.n_rows, tables.shape[-1]
+        b.max_rows = 1 if row_start is None else int(max_rows or 0)
+        b.max_len = int(max_len or 0)
+        b.row_start, b.kv_len, b.tables = _ptr(row_start), kv_len.data_ptr(), tables.data_ptr()
+        self._batch = b
+
+
+class KVPages:
+    """A pool of pages of K and V, in FP4 or bf16 (hermes_page_pool).
+
+    `pages`: uint8 [n_pages][page bytes] to use as the pool (allocated here if None).
+    The calls run on the current stream of the pool's device.  `faults()` reads and
+    clears the PAGE_BAD_* bits that calls have noted."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_rows: int = 64,
+                 fmt: int = PAGE_FP4, sm_scale: Optional[float] = None, rope_theta: float = 1.0e6, rope_axes: int = 1,
+                 mrope_section: Sequence[int] = (0, 0, 0), device: str = "cuda", pages: Optional[torch.Tensor] = None):
+        p = PagePoolStruct()
+        p.n_q_heads, p.n_kv_heads, p.head_dim, p.format = n_q_heads, n_kv_heads, head_dim, fmt
+        p.page_rows, p.n_pages = page_rows, n_pages
+        p.sm_scale = sm_scale if sm_scale is not None else 0.0
+        p.rope_theta, p.rope_axes = rope_theta, rope_axes
+        for i in range(3):
+            p.mrope_section[i] = int(mrope_section[i])
+        self.page_bytes = lib.hermes_page_bytes(ctypes.byref(p))
+        if self.page_bytes == 0:
+            raise HermesError(EINVAL, "hermes_page_bytes")
+        self.Hq, self.Hkv, self.d, self.axes = n_q_heads, n_kv_heads, head_dim, 3 if rope_axes == 3 else 1
+        if pages is None:
+            pages = torch.empty((n_pages, self.page_bytes), dtype=torch.uint8, device=device)
+        _need(pages, torch.uint8, (n_pages, self.page_bytes), "pages")
+        self.pages, self.device = pages, pages.device
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        p.pages, p.status = pages.data_ptr(), self._status.data_ptr()
+        self._pool = p
+
+    def _here(self, *tensors):
+        """The pool's device made current; every tensor has to be on it."""
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"a tensor on {t.device}, the pages are on {self.device}")
+        return torch.cuda.device(self.device)
+
+    def _rows(self, t: torch.Tensor, n: int, heads: int, name: str) -> int:
+        """Stride of rows [heads][d] of a bf16 device tensor that may lie apart."""
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or tuple(t.shape) != (n, heads, self.d):
+            raise ValueError(f"{name}: expected torch.bfloat16 {(n, heads, self.d)}, got "
+                             f"{getattr(t, 'dtype', None)} {tuple(getattr(t, 'shape', ()))}")
+        if not t.is_cuda or (n > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.d))):
+            raise ValueError(f"{name}: must be a device tensor of contiguous rows")
+        return t.stride(0) if n > 1 else heads * self.d
+
+    def append(self, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+               rope: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Rotates k (and q) to the positions `rope` (int32 [n_rows], or [3][n_rows]),
+        stores k and v as the last rows of their sequences, and returns the rotated q."""
+        n = batch.n_rows
+        ks, vs = self._rows(k, n, self.Hkv, "k"), self._rows(v, n, self.Hkv, "v")
+        qs = 0
+        if q is not None:
+            qs = self._rows(q, n, self.Hq, "q")
+            if q_out is None:
+                q_out = torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=self.device)
+            _need(q_out, torch.bfloat16, (n, self.Hq, self.d), "q_out")
+        if rope is not None:
+            _need(rope, torch.int32, (n,) if self.axes == 1 else (3, n), "rope")
+        with self._here(k, v, q, q_out, rope, batch.kv_len):
+            check(lib.hermes_page_append(ctypes.byref(self._pool), ctypes.byref(batch._batch), _ptr(q), qs, k.data_ptr(), ks,
+                                         v.data_ptr(), vs, _ptr(rope), _ptr(q_out), _stream()), "hermes_page_append")
+        return q_out
+
+    def attend(self, batch: PageBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Causal attention of every sequence's rows over its pages; lse: fp32
+        [n_rows][n_q_heads], written if given."""
+        n = batch.n_rows
+        qs = self._rows(q, n, self.Hq, "q")
+        if out is None:
+            out = torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=self.device)
+        _need(out, torch.bfloat16, (n, self.Hq, self.d), "out")
+        if lse is not None:
+            _need(lse, torch.float32, (n, self.Hq), "lse")
+        with self._here(q, out, lse, batch.kv_len):
+            nbytes = lib.hermes_page_workspace_bytes(ctypes.byref(self._pool), ctypes.byref(batch._batch))
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+            check(lib.hermes_page_attend(ctypes.byref(self._pool), ctypes.byref(batch._batch), q.data_ptr(), qs,
+                                         out.data_ptr(), _ptr(lse), _ptr(ws), nbytes, _stream()), "hermes_page_attend")
+        return out
+
+    def read(self, batch: PageBatch, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        """The stored (k, v) of the batch's rows, bf16 [n_rows][n_kv_heads][d]."""
+        shape = (batch.n_rows, self.Hkv, self.d)
+        if k is None:
+            k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        if v is None:
+            v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        _need(k, torch.bfloat16, shape, "k")
+        _need(v, torch.bfloat16, shape, "v")
+        with self._here(k, v, batch.kv_len):
+            check(lib.hermes_page_read(ctypes.byref(self._pool), ctypes.byref(batch._batch), k.data_ptr(), v.data_ptr(),
+                                       _stream()), "hermes_page_read")
+        return k, v
+
+    def faults(self) -> int:
+        bits = int(self._status.item())
+        self._status.zero_()
+        return bits
 
 
 def default_sm_scale(head_dim: int) -> float:
