@@ -1,25 +1,21 @@
 // Causal attention over pages for gfx950 (MFMA bf16, 64-wide waves).
 //
-// page_attn_few   a few packed rows (row, query head of the KV head) against
-//                 all keys of their sequence, or of a range of them
-// page_combine    joins the ranges
+// page_attn_few    up to 32 packed rows (row, query head of the KV head) an item
+// page_attn_many   256 packed rows an item
+// page_combine     joins the parts of items that were cut
 //
 // S = scale q k^T over the keys a row sees, O = softmax(S) V, in one pass over the
 // keys with a running maximum and sum (fp32), lse = ln sum exp S.
 //
-// MFMA layout (v_mfma_f32_16x16x32_bf16): lane l = 16 u + n supplies A[m = n][k = 8 u
-// .. + 7] and B[k = 8 u .. + 7][n]; result register j holds D[m = 4 u + j][n].
-//
-// A wave takes 32 keys a step, as two groups of 16, straight from the page into
-// registers: no LDS and no barrier between steps.
-//   S^T = K Q^T: lane (u, n) holds key n of a group and a quarter u of its channels.
-//   The k index of an MFMA may be any order of the channels that K and Q agree on,
-//   so with FP4 a lane's channels are one run, 16 bytes, one block with one scale.
-//   The result gives lane (u, n) row n and the keys 4 u .. 4 u + 3 of both groups.
-//   O^T = V^T P^T: those eight keys are the lane's k index of the second product, so P
-//   goes from one MFMA to the next without leaving its lane, and V comes as four
-//   rows' pieces of d / 16 channels, again 16 bytes a lane and group (FP4, d 128).
-// Both loads of a group are one contiguous KiB of the page.
+// The cut.  Lengths and rows are on the device and ragged, so the cut is made there:
+// every workgroup (unit) adds up the items' costs and takes an equal run of them,
+// [u q, (u + 1) q) of N with q = ceil(N / units).  The cost of item i of a
+// (sequence, KV head) pair is, in 1/G keys, G max(T - n, 0) + min((i + 1) rows, n G)
+// + kItemKeys G: the keys its last row sees, and a constant for its start and end.
+// That is an arithmetic progression, so the sums over a sequence's items, and the
+// item that holds a point, need no loop over items.  A cut inside an item falls on a
+// multiple of the step.  Items that lie in one unit are written at once; of a cut
+// item each unit leaves a part (fp32), at most two a unit.
 #include <type_traits>
 
 #include "pages_internal.h"
@@ -32,7 +28,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int NT = 256, NW = NT / 64;
-constexpr int KS = 32;                  // keys of a wave's step
+constexpr int KS = 32;                  // keys of a wave's step (page_attn_few)
 constexpr float kLowest = -3.0e38f;     // running maximum before the first key (finite: -inf minus it stays -inf)
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -53,6 +49,174 @@ __device__ __forceinline__ uint32_t fp4_pair(uint32_t codes, float scale, int by
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
+// ---------------------------------------------------------------------- the cut
+constexpr int kItemKeys = 128;          // what an item's start and end cost, in keys
+
+struct Item {
+  PageSeq seq;
+  int b, kv;
+  int64_t P, p0;            // packed rows of the sequence, the item's first
+  int64_t start, end;       // where the item lies in the run of all items
+};
+
+// A sequence's costs: sum(i) of its first i items a KV head.
+struct SeqCost {
+  int64_t base, P, rows, items;
+  __device__ __forceinline__ SeqCost(const PageSeq &s, int G, int rows_) {
+    base = (int64_t)G * (max(s.len - s.n, 0) + kItemKeys);
+    P = (int64_t)s.n * G;
+    rows = rows_;
+    items = (P + rows - 1) / rows;
+  }
+  __device__ __forceinline__ int64_t sum(int64_t i) const {
+    if (i < items) return i * base + rows * (i * (i + 1) / 2);
+    return items == 0 ? 0 : items * base + rows * (items * (items - 1) / 2) + P;
+  }
+};
+
+__device__ __forceinline__ int64_t shfl64(int64_t x, int lane) {
+  const uint32_t lo = __shfl((int)(uint32_t)x, lane), hi = __shfl((int)(x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t scalar64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The items of a call, a sequence a lane.
+struct Items {
+  const PagePool &pool;
+  const PageSeqs &seqs;
+  int rows, G;
+  __device__ __forceinline__ Items(const PageAttnArgs &a)
+      : pool(a.pool), seqs(a.seqs), rows(a.plan.rows), G(a.pool.Hq / a.pool.Hkv) {}
+  // inclusive sums of the costs of sequences b0 ..
+  __device__ __forceinline__ int64_t scan(int b0) const {
+    const int lane = threadIdx.x & 63;
+    int64_t x = 0;
+    if (b0 + lane < seqs.n_seqs) {
+      const SeqCost c(page_seq(pool, seqs, b0 + lane), G, rows);
+      x = pool.Hkv * c.sum(c.items);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t y = shfl64(x, max(lane - o, 0));
+      if (lane >= o) x += y;
+    }
+    return x;
+  }
+  __device__ __forceinline__ int64_t total() const {
+    int64_t n = 0;
+    for (int b = 0; b < seqs.n_seqs; b += 64) n += scalar64(shfl64(scan(b), 63));
+    return n;
+  }
+  // The item that holds x (x < total).
+  __device__ __forceinline__ Item find(int64_t x) const {
+    int64_t before = 0;
+    int b = 0;
+    for (;; b += 64) {
+      const int64_t sums = scan(b);
+      const unsigned long long past = __ballot(before + sums > x);
+      if (past != 0ull || b + 64 >= seqs.n_seqs) {
+        const int l = past != 0ull ? __builtin_ctzll(past) : 63;
+        before += l > 0 ? scalar64(shfl64(sums, l - 1)) : 0;
+        b += l;
+        break;
+      }
+      before += scalar64(shfl64(sums, 63));
+    }
+    return in_sequence(b, before, x);
+  }
+  // The item that holds x, in sequence b, whose items start at `before`.
+  __device__ __forceinline__ Item in_sequence(int b, int64_t before, int64_t x) const {
+    Item it;
+    it.b = b;
+    PageSeq s = page_seq(pool, seqs, b);
+    s.r0 = __builtin_amdgcn_readfirstlane(s.r0);
+    s.n = __builtin_amdgcn_readfirstlane(s.n);
+    s.len = __builtin_amdgcn_readfirstlane(s.len);
+    it.seq = s;
+    const SeqCost c(s, G, rows);
+    it.P = c.P;
+    const int64_t head = c.sum(c.items);
+    int64_t rest = x - before;
+    it.kv = 0;
+    if (pool.Hkv > 1) {
+      it.kv = (int)scalar64(rest / head);
+      rest -= it.kv * head;
+    }
+    int64_t i = 0, j = c.items;           // sum(i) <= rest < sum(j)
+    while (j - i > 1) {
+      const int64_t m = (i + j) / 2;
+      if (c.sum(m) <= rest) i = m; else j = m;
+    }
+    it.p0 = i * rows;
+    it.start = before + it.kv * head + c.sum(i);
+    it.end = before + it.kv * head + c.sum(i + 1);
+    return it;
+  }
+  // The item after `it`, if any (it.end < total).
+  __device__ __forceinline__ Item next(const Item &it) const {
+    const SeqCost c(it.seq, G, rows);
+    const int64_t all = pool.Hkv * c.sum(c.items), head = c.sum(c.items);
+    const int64_t before = it.start - it.kv * head - c.sum(it.p0 / rows);
+    if (it.end < before + all) return in_sequence(it.b, before, it.end);
+    int b = it.b + 1;                      // (sequences without rows have no items)
+    while (b + 1 < seqs.n_seqs && __builtin_amdgcn_readfirstlane(page_seq(pool, seqs, b).n) == 0) ++b;
+    return in_sequence(b, it.end, it.end);
+  }
+};
+
+// A unit's walk over its items: body(item, lo, hi, whole, slot) for each, with the keys
+// [lo, hi) of it that are the unit's.
+template <typename F>
+__device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&body) {
+  const Items items(a);
+  const int G = items.G, step = a.plan.step;
+  const int64_t N = items.total();
+  int64_t q = (N + a.plan.units - 1) / a.plan.units;
+  q = scalar64(max(q, (int64_t)step * G));
+  const int64_t lo = unit * q, hi = min(lo + q, N);
+  PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
+  if (lo < hi) {
+    Item it = items.find(lo);
+    if (it.start < lo && it.start >= lo - q)    // this unit holds the item's first cut
+      cut = PageCut{unit - 1, (int)((it.end - 1) / q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, 0, it.p0, it.P};
+    for (int slot = 0;; slot = 1) {
+      // the keys its last row sees
+      const int last = (int)((min(it.p0 + a.plan.rows, it.P) - 1) / G);
+      const int end = max(0, it.seq.len - it.seq.n + last + 1);
+      auto key_at = [&](int64_t x) { return (int)min((x - it.start) / G / step * step, (int64_t)end); };
+      const int k0 = it.start >= lo ? 0 : key_at(lo), k1 = it.end <= hi ? end : key_at(hi);
+      body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), it.start >= lo && it.end <= hi, slot);
+      if (it.end >= hi) break;
+      it = items.next(it);
+    }
+  }
+  if (a.plan.units > 1 && threadIdx.x == 0) a.cuts[unit] = cut;
+}
+
+// Workgroups are dispatched to the 8 XCDs round-robin; consecutive units, which read
+// the same sequence, are given to the same XCD, and share its L2.
+__device__ __forceinline__ int xcd_remap(int i, int n) {
+  const int q = n / 8, r = n % 8, x = i % 8, k = i / 8;
+  return x < r ? x * (q + 1) + k : r * (q + 1) + (x - r) * q + k;
+}
+
+// ------------------------------------------------------------------- a few rows
+// MFMA layout (v_mfma_f32_16x16x32_bf16): lane l = 16 u + n supplies A[m = n][k = 8 u
+// .. + 7] and B[k = 8 u .. + 7][n]; result register j holds D[m = 4 u + j][n].
+//
+// A wave takes 32 keys a step, as two groups of 16, straight from the page into
+// registers: no LDS and no barrier between steps.
+//   S^T = K Q^T: lane (u, n) holds key n of a group and a quarter u of its channels.
+//   The k index of an MFMA may be any order of the channels that K and Q agree on,
+//   so with FP4 a lane's channels are one run, 16 bytes, one block with one scale.
+//   The result gives lane (u, n) row n and the keys 4 u .. 4 u + 3 of both groups.
+//   O^T = V^T P^T: those eight keys are the lane's k index of the second product, so P
+//   goes from one MFMA to the next without leaving its lane, and V comes as four
+//   rows' pieces of d / 16 channels, again 16 bytes a lane and group (FP4, d 128).
+// Both loads of a group are one contiguous KiB of the page.
 // What a lane holds of a step's 32 keys, as it lies in the page: WK words of K and
 // WV of V for each group of 16 keys, and with FP4 the scales.
 template <int D, bool FP4>
@@ -70,6 +234,8 @@ __device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *p) {
       const uint4 x = reinterpret_cast<const uint4 *>(p)[i];
       w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
     }
+  } else if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t *>(p);
   } else {
     static_assert(N == 2, "two words");
     const uint2 x = *reinterpret_cast<const uint2 *>(p);
@@ -83,15 +249,11 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
   constexpr int KK = D / 32;                // MFMAs of S for each group of keys
   constexpr int PC = D / 16;                // channels of a piece of V
   const PagePool &pool = a.pool;
-  const int Hq = pool.Hq, Hkv = pool.Hkv, G = Hq / Hkv;
-  const int split = blockIdx.x % a.plan.splits, pair = blockIdx.x / a.plan.splits;
-  const int kv = pair % Hkv, b = pair / Hkv;
-  const PageSeq seq = page_seq(pool, a.seqs, b);
+  const int Hq = pool.Hq, G = Hq / pool.Hkv;
+  const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n16 = lane & 15, u = lane >> 4;
-  const int64_t P = (int64_t)seq.n * G;
   const int rows_log = pool.log_rows, page_rows = 1 << rows_log;
-  const int32_t *table = a.seqs.tables + (int64_t)b * a.seqs.max_pages;
   const float c = a.scale_log2, inv_c = 1.f / c;
 
   // lane's byte offsets in a KV head's block, from the first row of a group of 16
@@ -103,13 +265,13 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
   __shared__ __attribute__((aligned(16))) float so[NW][16][D + 4];
   __shared__ float2 sml[NW][16];
 
-  for (int64_t p0 = (int64_t)blockIdx.y * (16 * RT); p0 < P; p0 += (int64_t)gridDim.y * (16 * RT)) {
-    // keys [lo, hi) of this range; row i of the tile sees those below base + i + 1
-    const int first = (int)(p0 / G), last = (int)((min(p0 + 16 * RT, P) - 1) / G);
-    const int base = seq.len - seq.n;
-    const int end = max(0, base + last + 1);
-    const int lo = (int)min((int64_t)split * a.plan.range, (int64_t)end);
-    const int hi = split == a.plan.splits - 1 ? end : lo + min(end - lo, a.plan.range);
+  walk_items(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
+    // keys [lo, hi); row i of the sequence sees those below base + i + 1
+    const PageSeq seq = it.seq;
+    const int kv = it.kv;
+    const int64_t p0 = it.p0, P = it.P;
+    const int first = (int)(p0 / G), base = seq.len - seq.n;
+    const int32_t *table = a.seqs.tables + (int64_t)it.b * a.seqs.max_pages;
 
     bf16x8 qf[RT][KK];
     int vis[RT];                            // keys this lane's row sees
@@ -313,7 +475,7 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
       }
     }
 
-    // join the waves, 16 rows at a time: thread (row, piece of eight channels)
+    // join the waves' states, 16 rows at a time: thread (row, piece of eight channels)
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (p0 + 16 * t >= P) break;
@@ -348,13 +510,13 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
       }
       const int i = (int)(p / G), g = (int)(p - (int64_t)i * G);
       const int64_t at = (int64_t)(seq.r0 + i) * Hq + kv * G + g;
-      if (a.plan.splits > 1) {
-        const int64_t blk = (int64_t)split * ((int64_t)a.seqs.n_rows * Hq) + at;
-        if (piece == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * blk) = float2{m, sum};
-        if (hi > lo) {                      // (an empty range leaves its O unwritten, and unread)
+      if (!whole) {
+        const int64_t at2 = (int64_t)(2 * unit + slot) * (16 * RT) + 16 * t + row;
+        if (piece == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * at2) = float2{m, sum};
+        if (hi > lo) {                      // (an empty part leaves its O unwritten, and unread)
 #pragma unroll
           for (int x = 0; x < PC; x += 4)
-            *reinterpret_cast<float4 *>(a.opart + blk * D + PC * piece + x) =
+            *reinterpret_cast<float4 *>(a.opart + at2 * D + PC * piece + x) =
                 float4{acc[x], acc[x + 1], acc[x + 2], acc[x + 3]};
         }
       } else {
@@ -366,76 +528,411 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
         if (a.lse != nullptr && piece == 0) a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
       }
     }
-    __syncthreads();   // so and sml are free for the next tile
-  }
+    __syncthreads();   // so and sml are free for the next item
+  });
 }
 
-// Joins the ranges of a row: O = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).
-// A wave takes one (row, query head).
-template <int D>
-__global__ __launch_bounds__(NT) void page_combine(PageAttnArgs a) {
+// ------------------------------------------------------------------- many rows
+// MFMA layout (v_mfma_f32_32x32x16_bf16): lane l supplies A[m = l % 32][k = 8 (l / 32)
+// .. + 7] and B[k = 8 (l / 32) .. + 7][n = l % 32]; result register j of lane l holds
+// D[m = 8 (j / 4) + 4 (l / 32) + j % 4][n = l % 32].
+//
+// Eight waves of 32 packed rows share every tile of 64 keys: each wave fetches eight
+// keys' K and V from the page (so a page id is a scalar, and a KV head's 4 bits cost
+// a workgroup 8.5 KB a tile), turns FP4 into bf16 on the way to LDS, and all read
+// the tile from there, K row by row and V transposed by ds_read_b64_tr_b16.  As in
+// attn_fwd, S^T = K Q^T puts one query row a lane, so the softmax stays in the lane and
+// P^T is the B operand of O^T = V^T P^T as it is.
+constexpr int MT = 512, MW = MT / 64;   // waves
+constexpr int MROWS = 32 * MW;          // packed rows of an item
+constexpr int MK = 64;                  // keys of a tile
+constexpr int KPAD = 8, VPAD = 32;      // u16 padding of K and V rows in LDS
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Inside each group of 16 lanes, lane j receives element j % 4 of the 8-byte rows
+// addressed by lanes j / 4, 4 + j / 4, 8 + j / 4, 12 + j / 4.
+__device__ __forceinline__ s4 lds_tr16(const uint16_t *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
+}
+
+template <int D, bool FP4>
+__global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
+  using B = PageBlock<D, FP4>;
+  constexpr int WKEYS = MK / MW;          // keys a wave fetches
+  constexpr int UK = WKEYS * D / 8 / 64;  // pieces of eight channels of K a lane fetches
+  constexpr int LK = D / 8 / UK;          // lanes of a key
+  constexpr int PC = D / 16;              // channels of a piece of V; a lane fetches one of two keys
+  static_assert(WKEYS / 4 * 16 * 2 == 64, "two keys' piece of V a lane");
+  constexpr int WK = FP4 ? UK : 4 * UK, WV = FP4 ? D / 64 : D / 16;   // words a lane fetches
+  constexpr int kAheadK = 4, kAheadV = 4; // LDS reads issued ahead of their MFMA
+
+  const PagePool &pool = a.pool;
+  const int Hq = pool.Hq, G = Hq / pool.Hkv;
+  const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int Hq = a.pool.Hq, S = a.plan.splits;
-  const int64_t total = (int64_t)a.seqs.n_rows * Hq;
-  const int per = gridDim.x / a.seqs.n_seqs;    // workgroups of a sequence
-  const PageSeq seq = page_seq(a.pool, a.seqs, blockIdx.x / per);
-  const int64_t n = (int64_t)seq.n * Hq;
-  for (int64_t x = (int64_t)(blockIdx.x % per) * NW + wave; x < n; x += (int64_t)per * NW) {
-    const int64_t at = (int64_t)seq.r0 * Hq + x;
-    float m = kLowest, l = 0.f;
-    float2 acc = {0.f, 0.f};
-    for (int s0 = 0; s0 < S; s0 += 64) {
-      // lane s has range s0 + s's (max, sum)
-      float2 ml = {kLowest, 0.f};
-      if (s0 + lane < S) ml = *reinterpret_cast<const float2 *>(a.mlpart + 2 * ((s0 + lane) * total + at));
-      float mn = ml.x;
+  const int half = lane >> 5, l32 = lane & 31;
+  const int rows_log = pool.log_rows, page_rows = 1 << rows_log;
+  const float c = a.scale_log2, inv_c = 1.f / c;
+
+  // what this lane fetches: of key `kkey` of the wave's eight, channels 8 kpc ..; of keys
+  // vkey and vkey + 1, channels PC vpc ..
+  const int kkey = lane / LK, kpc = lane % LK * UK;
+  const int vpc = lane % 32 / 2, vkey = lane / 32 * 4 + lane % 2 * 2;
+  const int k_ofs = B::k(kkey) + kpc * (FP4 ? 4 : 16);
+  const int v_ofs = B::v(page_rows, lane / 32) + vpc * 4 * B::kPiece + lane % 2 * 2 * B::kPiece;
+  const int ks_ofs = B::ks(page_rows, kkey) + kpc * 8 / 32;
+  const int vs_ofs = B::vs(page_rows, lane / 32) + vpc * PC / 32 * 4 + lane % 2 * 2;
+
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[2][MK][D + KPAD];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[2][MK][D + VPAD];
+  // transposed-read coordinates of this lane inside its 16-lane group
+  const int tr_row = 4 * half + ((lane & 15) >> 2);
+  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+
+  walk_items(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
+    const PageSeq seq = it.seq;
+    const int kv = it.kv;
+    const int64_t p0 = it.p0, P = it.P;
+    const int first = (int)(p0 / G), base = seq.len - seq.n;
+    const int all_see = base + first + 1;   // keys that every row of the item sees
+    const int32_t *table = a.seqs.tables + (int64_t)it.b * a.seqs.max_pages;
+    const uint8_t *blocks = pool.pages + (int64_t)kv * pool.block_bytes;
+
+    // this lane's query row
+    const int64_t p = p0 + 32 * wave + l32;
+    const bool row_ok = p < P;
+    const bool wave_rows = p0 + 32 * wave < P;    // (a wave without rows still fetches)
+    const int r = row_ok ? (int)(p / G) : 0, g = row_ok ? (int)(p - (int64_t)r * G) : 0;
+    const int vis = row_ok ? base + r + 1 : 0;    // keys it sees
+    const int64_t at = (int64_t)(seq.r0 + r) * Hq + kv * G + g;
+    bf16x8 qf[D / 16];
+    {
+      const uint16_t *q = a.q + (int64_t)(seq.r0 + r) * a.q_stride + (int64_t)(kv * G + g) * D + 8 * half;
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor(mn, o));
-      mn = fmaxf(mn, m);
-      const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - mn);
-      float ls = w * ml.y;
+      for (int kk = 0; kk < D / 16; ++kk) qf[kk] = row_ok ? *reinterpret_cast<const bf16x8 *>(q + 16 * kk) : bf16x8{};
+    }
+    f32x16 o[D / 32];
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) ls += __shfl_xor(ls, o);
-      const float old = fast_exp2(m - mn);
-      l = l * old + ls;
-      acc.x *= old;
-      acc.y *= old;
-      m = mn;
-      unsigned long long live = __ballot(ml.y != 0.f);
-      while (live != 0ull) {
-        const int s = __builtin_ctzll(live);
-        live &= live - 1;
-        const float ws = __shfl(w, s);
-        const float *op = a.opart + ((s0 + s) * total + at) * D;
-        if constexpr (D == 128) {
-          const float2 y = *reinterpret_cast<const float2 *>(op + 2 * lane);
-          acc.x += ws * y.x;
-          acc.y += ws * y.y;
-        } else {
-          acc.x += ws * op[lane];
+    for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
+    float m_run = kLowest, l_run = 0.f;
+    float m_lim = (kLowest + 8.f) * inv_c;
+
+    // lane x holds the page of this wave's keys of tile t0 + x (-1: none)
+    const int t_hi = (hi + MK - 1) / MK, t_lo = lo < hi ? lo / MK : t_hi;   // (an empty part starts anywhere)
+    int ids = -1, ids_at = t_lo;
+    auto find_pages = [&](int t) {
+      ids_at = t;
+      const int64_t key = (int64_t)(t + lane) * MK + wave * WKEYS;
+      ids = -1;
+      if (t + lane < t_hi && key < hi) {
+        ids = table[key >> rows_log];
+        if (ids < 0 || ids >= pool.n_pages) {
+          ids = -1;
+          page_note(pool, HERMES_PAGE_BAD_ID);
         }
       }
+    };
+    uint32_t kw[WK], vw[WV], ksc = 0, vsc = 0;
+    auto load = [&](int t) {
+      if (t - ids_at >= 64) find_pages(t);
+      const int id = __builtin_amdgcn_readlane(ids, t - ids_at);
+      const int key0 = t * MK + wave * WKEYS, row = key0 & (page_rows - 1);
+      const uint8_t *block = blocks + (int64_t)max(id, 0) * pool.page_bytes;
+      load_words<WK>(kw, block + row * B::kRow + k_ofs);
+      load_words<WV>(vw, block + row * B::kRow + v_ofs);
+      if constexpr (FP4) {
+        ksc = *(block + row * B::kScales + ks_ofs);
+        vsc = *reinterpret_cast<const uint16_t *>(block + row * B::kScales + vs_ofs);
+      }
+      // what lies past the length, or in no page, may be anything: zeros instead
+      if (__builtin_expect(id < 0 || key0 + WKEYS > seq.len, 0)) {
+        const int valid = id < 0 ? 0 : seq.len - key0;
+        if (kkey >= valid) {
+          ksc = 0;
+#pragma unroll
+          for (int i = 0; i < WK; ++i) kw[i] = 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (vkey + j < valid) continue;
+          if constexpr (FP4) {
+            vsc &= ~(0xFFu << (8 * j));
+            if constexpr (D == 128) vw[j] = 0u;
+            else vw[0] &= j == 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          } else {
+#pragma unroll
+            for (int i = 0; i < WV / 2; ++i) vw[j * (WV / 2) + i] = 0u;
+          }
+        }
+      }
+    };
+    auto store_tile = [&](int b) {
+      uint16_t *kd = &Ks[b][wave * WKEYS + kkey][kpc * 8];
+      const float sc = scale_of(ksc);
+#pragma unroll
+      for (int i = 0; i < UK; ++i) {
+        uint4 x;
+        if constexpr (FP4) x = uint4{fp4_pair(kw[i], sc, 0), fp4_pair(kw[i], sc, 1), fp4_pair(kw[i], sc, 2), fp4_pair(kw[i], sc, 3)};
+        else x = uint4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]};
+        *reinterpret_cast<uint4 *>(kd + 8 * i) = x;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint16_t *vd = &Vs[b][wave * WKEYS + vkey + j][vpc * PC];
+        const float vs = scale_of(j == 0 ? vsc & 0xFFu : vsc >> 8);
+        if constexpr (D == 128) {
+          uint4 x;
+          if constexpr (FP4) x = uint4{fp4_pair(vw[j], vs, 0), fp4_pair(vw[j], vs, 1), fp4_pair(vw[j], vs, 2), fp4_pair(vw[j], vs, 3)};
+          else x = uint4{vw[4 * j], vw[4 * j + 1], vw[4 * j + 2], vw[4 * j + 3]};
+          *reinterpret_cast<uint4 *>(vd) = x;
+        } else {
+          uint2 x;
+          if constexpr (FP4) x = uint2{fp4_pair(vw[0], vs, 2 * j), fp4_pair(vw[0], vs, 2 * j + 1)};
+          else x = uint2{vw[2 * j], vw[2 * j + 1]};
+          *reinterpret_cast<uint2 *>(vd) = x;
+        }
+      }
+    };
+    auto compute = [&](int b, int t, auto masked) {
+      f32x16 s[2];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        s[sub] = f32x16{};
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          s[sub] = mfma32(*reinterpret_cast<const bf16x8 *>(&Ks[b][sub * 32 + l32][16 * kk + 8 * half]), qf[kk], s[sub]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAheadK; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * (D / 16) - kAheadK; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAheadK; ++i) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if constexpr (decltype(masked)::value) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+          for (int jj = 0; jj < 16; ++jj)
+            if (t * MK + sub * 32 + 8 * (jj >> 2) + 4 * half + (jj & 3) >= vis) s[sub][jj] = -INFINITY;
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+        for (int jj = 0; jj < 16; ++jj) mx = fmaxf(mx, s[sub][jj]);
+      }
+      {
+        // a row's keys are split over the lane halves
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        const float m0 = __uint_as_float(x[0]), m1 = __uint_as_float(x[1]);
+        mx = m0 > m1 ? m0 : m1;
+      }
+      // the maximum moves only when it is passed by more than 2^8 (log2 domain)
+      if (__builtin_expect(__any(mx > m_lim), 0)) {
+        const float m_new = fmaxf(m_run, mx * c);
+        const float alpha = fast_exp2(m_run - m_new);
+        m_run = m_new;
+        m_lim = (m_run + 8.f) * inv_c;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
+      }
+      bf16x8 pf[4];
+      float ls = 0.f;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+        for (int jj = 0; jj < 16; ++jj) {
+          const float x = fast_exp2(fmaf(s[sub][jj], c, -m_run));
+          ls += x;
+          pf[2 * sub + (jj >> 3)][jj & 7] = static_cast<__bf16>(x);   // (P enters an MFMA as bf16; the sum keeps fp32)
+        }
+      }
+      l_run += ls;
+      __builtin_amdgcn_s_setprio(1);        // (the SIMD's other wave fills in with its softmax)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+#pragma unroll
+        for (int qq = 0; qq < 4; ++qq) {
+          const uint16_t *vp = &Vs[b][16 * qq + tr_row][32 * db + tr_col];
+          const s4 x = lds_tr16(vp), y = lds_tr16(vp + 8 * (D + VPAD));
+          o[db] = mfma32(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7)), pf[qq], o[db]);
+        }
+      }
+      constexpr int kPV = D / 32 * 4;
+#pragma unroll
+      for (int i = 0; i < 2 * kAheadV; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+#pragma unroll
+      for (int i = 0; i < kPV - kAheadV; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+#pragma unroll
+      for (int i = 0; i < kAheadV; ++i) __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    using Masked = std::integral_constant<bool, true>;
+    using Open = std::integral_constant<bool, false>;
+    __syncthreads();                        // the tiles of the item before are read
+    if (t_lo < t_hi) {
+      find_pages(t_lo);
+      load(t_lo);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if constexpr (D == 128)
-      *reinterpret_cast<uint32_t *>(a.out + at * D + 2 * lane) = f2bf(acc.x * inv) | f2bf(acc.y * inv) << 16;
-    else
-      a.out[at * D + lane] = (uint16_t)f2bf(acc.x * inv);
-    if (a.lse != nullptr && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    // tiles that every row sees whole, two a trip so that each LDS buffer is a constant
+    const int t_open = min(t_hi - 1, all_see / MK);
+    int t = t_lo;
+    for (; t + 1 < t_open; t += 2) {
+      store_tile(0);
+      __syncthreads();
+      load(t + 1);
+      if (wave_rows) compute(0, t, Open{});
+      store_tile(1);
+      __syncthreads();
+      load(t + 2);
+      if (wave_rows) compute(1, t + 1, Open{});
+    }
+    for (int b = 0; t < t_hi; ++t, b ^= 1) {
+      store_tile(b);
+      __syncthreads();
+      if (t + 1 < t_hi) load(t + 1);
+      if (!wave_rows) continue;
+      if ((t + 1) * MK > all_see) compute(b, t, Masked{});
+      else compute(b, t, Open{});
+    }
+
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (row_ok && !whole) {
+      const int64_t part = (int64_t)(2 * unit + slot) * MROWS + 32 * wave;
+      if (half == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * (part + l32)) = float2{m_run, l};
+      float4 *op = reinterpret_cast<float4 *>(a.opart + part * D) + lane;   // [channels / 8][lane]
+      if (hi > lo) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+          op[i * 64] = float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+      }
+    } else if (row_ok) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row sees nothing; a NaN stays one)
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        *reinterpret_cast<uint2 *>(a.out + at * D + 8 * i + 4 * half) =
+            uint2{f2bf(o[i / 4][4 * (i % 4)] * inv) | f2bf(o[i / 4][4 * (i % 4) + 1] * inv) << 16,
+                  f2bf(o[i / 4][4 * (i % 4) + 2] * inv) | f2bf(o[i / 4][4 * (i % 4) + 3] * inv) << 16};
+      if (a.lse != nullptr && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
+    }
+  });
+}
+
+// -------------------------------------------------------------------- the joins
+// O = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m) over the parts s of a cut
+// item.  Workgroup (u, y): item that unit u cut first, 64 float4 of its O; wave w
+// takes the parts w, w + 4, ..., four loaded at once, and the waves' sums are joined
+// in wave order.
+template <int D, bool MANY>
+__global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
+  const PageCut cut = a.cuts[blockIdx.x];
+  if (cut.last < cut.first) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // which row and channels float4 `i` of a part holds
+  const int i = blockIdx.y * 64 + lane;
+  int row, ch;
+  if constexpr (MANY) {     // [32 rows][channels / 8][lane]
+    row = i / (D / 8 * 64) * 32 + i % 32;
+    ch = i / 64 % (D / 8) * 8 + i / 32 % 2 * 4;
+  } else {
+    row = i / (D / 4);
+    ch = i % (D / 4) * 4;
   }
+  const int rows = a.plan.rows;
+  if (__all(cut.p0 + row >= cut.P)) return;
+  const int parts = cut.last - cut.first + 1;
+  auto part = [&](int s) { return (int64_t)2 * (cut.first + s) + (s == 0 ? cut.slot : 0); };
+  float m = kLowest, l = 0.f;
+  float4 acc = {0.f, 0.f, 0.f, 0.f};
+  constexpr int AHEAD = 4;
+  for (int s0 = wave; s0 < parts; s0 += 4 * AHEAD) {
+    float2 ml[AHEAD];
+    float4 o[AHEAD];
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) {
+      const int s = s0 + 4 * x;
+      ml[x] = float2{kLowest, 0.f};
+      o[x] = float4{0.f, 0.f, 0.f, 0.f};
+      if (s < parts && cut.p0 + row < cut.P) {
+        ml[x] = *reinterpret_cast<const float2 *>(a.mlpart + 2 * (part(s) * rows + row));
+        o[x] = reinterpret_cast<const float4 *>(a.opart + part(s) * rows * D)[i];
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) mn = fmaxf(mn, ml[x].x);
+    const float old = fast_exp2(m - mn);
+    m = mn;
+    l *= old;
+    acc = float4{acc.x * old, acc.y * old, acc.z * old, acc.w * old};
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) {
+      if (ml[x].y == 0.f) continue;        // (an empty part, whose O was not written)
+      const float w = fast_exp2(ml[x].x - m);
+      l += w * ml[x].y;
+      acc.x += w * o[x].x;
+      acc.y += w * o[x].y;
+      acc.z += w * o[x].z;
+      acc.w += w * o[x].w;
+    }
+  }
+  __shared__ float4 sacc[4][64];
+  __shared__ float2 sml[4][64];
+  sacc[wave][lane] = acc;
+  sml[wave][lane] = float2{m, l};
+  __syncthreads();
+  if (wave != 0 || cut.p0 + row >= cut.P) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = fmaxf(m, sml[w][lane].x);
+  float4 t = {0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float2 x = sml[w][lane];
+    const float4 y = sacc[w][lane];
+    const float e = fast_exp2(x.x - m);
+    l += e * x.y;
+    t.x += e * y.x;
+    t.y += e * y.y;
+    t.z += e * y.z;
+    t.w += e * y.w;
+  }
+  const int G = a.pool.Hq / a.pool.Hkv;
+  const int64_t p = cut.p0 + row;
+  const int r = (int)(p / G), g = (int)(p - (int64_t)r * G);
+  const int64_t at = (int64_t)(cut.r0 + r) * a.pool.Hq + cut.kv * G + g;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<uint2 *>(a.out + at * D + ch) =
+      uint2{f2bf(t.x * inv) | f2bf(t.y * inv) << 16, f2bf(t.z * inv) | f2bf(t.w * inv) << 16};
+  if (a.lse != nullptr && ch == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 template <int D, bool FP4>
 hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.plan.splits * a.pool.Hkv * a.seqs.n_seqs), a.plan.tiles);
-  if (a.plan.rows == 16) hipLaunchKernelGGL((page_attn_few<D, FP4, 1>), grid, dim3(NT), 0, s, a);
-  else if (a.plan.rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2>), grid, dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL((page_attn_few<D, FP4, 4>), grid, dim3(NT), 0, s, a);
+  const dim3 grid(a.plan.units);
+  const int rows = a.plan.rows;
+  if (rows == 16) hipLaunchKernelGGL((page_attn_few<D, FP4, 1>), grid, dim3(NT), 0, s, a);
+  else if (rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2>), grid, dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL((page_attn_many<D, FP4>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.plan.splits == 1) return e;
-  const int64_t rows = (int64_t)a.plan.tiles * a.plan.rows * a.pool.Hkv;   // (of a sequence, at least)
-  const int64_t per = min((rows + NW - 1) / NW, max((int64_t)1, (int64_t)(1 << 24) / a.seqs.n_seqs));
-  hipLaunchKernelGGL(page_combine<D>, dim3((unsigned)(per * a.seqs.n_seqs)), dim3(NT), 0, s, a);
+  if (e != hipSuccess || a.plan.units == 1) return e;
+  const dim3 joins(a.plan.units, rows * D / 256);
+  if (rows <= 64) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

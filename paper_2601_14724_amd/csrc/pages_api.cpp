@@ -27,6 +27,10 @@ int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
   if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
   if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
   if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;
+  // the cost of all items of an attention call has to fit 62 bits (items of 16 rows, one more a pair)
+  const double G = (double)p->n_q_heads / p->n_kv_heads, keys = (double)b->max_pages * p->page_rows;
+  const double items = (double)b->n_rows * p->n_q_heads / 16.0 + (double)b->n_seqs * p->n_kv_heads;
+  if (items * (G * (keys + 1024.0) + (double)b->n_rows * G) > 4.0e18) return HERMES_EINVAL;
   return HERMES_OK;
 }
 
@@ -55,22 +59,21 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t max_len = b->max_len > 0 && b->max_len < table ? b->max_len : table;
   const int64_t P = max_rows * G;
   PagePlan x;
-  x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 64;
-  const int64_t tiles = over(P, x.rows);
-  x.tiles = (int32_t)(tiles < 65535 ? tiles : 65535);
-  // two workgroups a CU, each of at least a step (of 32 keys) for its four waves
-  const int64_t pairs = (int64_t)b->n_seqs * p->n_kv_heads * x.tiles;
-  int64_t splits = 2 * kStreamSlots / pairs;
-  if (splits > over(max_len, 128)) splits = over(max_len, 128);
-  if (splits < 1) splits = 1;
-  x.range = (int32_t)(over(over(max_len, splits), 128) * 128);
-  x.splits = (int32_t)over(max_len, x.range);
+  x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 256;
+  x.step = x.rows <= 64 ? 128 : 64;
+  // no more units than steps, nor than fit the CUs (two workgroups of four waves, or
+  // one of eight)
+  const int64_t steps = (int64_t)b->n_seqs * p->n_kv_heads * over(P, x.rows) * over(max_len, x.step);
+  const int64_t slots = x.rows <= 64 ? 2 * kStreamSlots : kStreamSlots;
+  x.units = (int32_t)(steps < slots ? steps : slots);
   return x;
 }
 
-size_t workspace_of(const hermes_page_pool *p, const hermes_page_batch *b, const PagePlan &x) {
-  if (x.splits == 1) return 0;
-  return sizeof(float) * (size_t)x.splits * (size_t)b->n_rows * p->n_q_heads * (p->head_dim + 2);
+// Workspace: the cuts, then O and (max, sum) of 2 units parts.
+size_t cuts_bytes(const PagePlan &x) { return (sizeof(PageCut) * (size_t)x.units + 255) / 256 * 256; }
+size_t workspace_of(const hermes_page_pool *p, const PagePlan &x) {
+  if (x.units == 1) return 0;
+  return cuts_bytes(x) + sizeof(float) * 2 * (size_t)x.units * x.rows * (p->head_dim + 2);
 }
 
 void fill_rope(const hermes_page_pool *p, PageAppendArgs *a) {
@@ -142,7 +145,7 @@ size_t hermes_page_bytes(const hermes_page_pool *pool) {
 size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_page_batch *batch) {
   if (check_page_pool(pool) != HERMES_OK || check_batch(pool, batch) != HERMES_OK) return 0;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return 0;
-  return workspace_of(pool, batch, plan_of(pool, batch));
+  return workspace_of(pool, plan_of(pool, batch));
 }
 
 int hermes_page_append(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,
@@ -189,12 +192,13 @@ int hermes_page_attend(const hermes_page_pool *pool, const hermes_page_batch *ba
   PageAttnArgs a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan_of(pool, batch);
-  const size_t need = workspace_of(pool, batch, a.plan);
+  const size_t need = workspace_of(pool, a.plan);
   if (need > 0) {
     if (workspace == nullptr || !aligned(workspace, 16)) return HERMES_EINVAL;
     if (ws_bytes < need) return HERMES_ECAPACITY;
-    a.opart = static_cast<float *>(workspace);
-    a.mlpart = a.opart + (size_t)a.plan.splits * batch->n_rows * pool->n_q_heads * pool->head_dim;
+    a.cuts = static_cast<PageCut *>(workspace);
+    a.opart = reinterpret_cast<float *>(static_cast<char *>(workspace) + cuts_bytes(a.plan));
+    a.mlpart = a.opart + 2 * (size_t)a.plan.units * a.plan.rows * pool->head_dim;
   }
   a.pool = page_pool_of(pool);
   a.seqs = seqs_of(batch);

@@ -50,11 +50,23 @@ struct PagePackArgs {
   int32_t len[kMaxLayers];
 };
 
-// How an attention call is cut: tiles of `rows` packed rows (row, query head of
-// the KV head), and `splits` ranges of `range` keys each (the last one up to the
-// end, however long).
+// How an attention call is cut.  An item is a tile of `rows` packed rows (row, query
+// head of the KV head) of one (sequence, KV head), against all keys its rows see.
+// The items, in order, are cut into `units` runs of equal cost, a workgroup each, at
+// least `step` keys long: the lengths are on the device, so the kernel finds its run.
+// rows up to 64 take page_attn_few, more page_attn_many.
 struct PagePlan {
-  int32_t rows, splits, range, tiles;
+  int32_t rows, units, step;
+};
+
+// What page_combine has to know of a cut item, written by the unit that holds its
+// first cut: the units that have parts of it, its first packed row and its rows.
+struct PageCut {
+  int32_t first, last;      // units (last < first: no item is first cut here)
+  int32_t slot;             // of the first unit's part: 0 or 1 (the others: 0)
+  int32_t kv, r0;           // KV head, first stacked row of the sequence
+  int32_t pad_;
+  int64_t p0, P;            // the item's first packed row, the sequence's packed rows
 };
 
 struct PageAttnArgs {
@@ -66,8 +78,12 @@ struct PageAttnArgs {
   float *lse;               // [n_rows][Hq] or null
   float scale_log2;         // sm_scale * log2(e)
   PagePlan plan;
-  float *opart;             // splits > 1: [splits][n_rows * Hq][d] unnormalised O
-  float *mlpart;            // [splits][n_rows * Hq][2] (max, sum), log2 domain
+  // Parts of cut items: unit u has two, 2 u for the item it starts with and 2 u + 1
+  // for the one it ends with, each rows x d fp32 (unnormalised O) and (max, sum) pairs
+  // (log2 domain).
+  PageCut *cuts;            // [units]
+  float *opart;
+  float *mlpart;
 };
 
 hipError_t launch_page_append(const PageAppendArgs &a, int head_dim, int format, hipStream_t s);
