@@ -55,7 +55,7 @@ constexpr int kItemKeys = 128;          // what an item's start and end cost, in
 struct Item {
   PageSeq seq;
   int b, kv;
-  int64_t P, p0;            // packed rows of the sequence, the item's first
+  int P, p0;                // packed rows of the sequence, the item's first
   int64_t start, end;       // where the item lies in the run of all items
 };
 
@@ -137,7 +137,7 @@ struct Items {
     s.len = __builtin_amdgcn_readfirstlane(s.len);
     it.seq = s;
     const SeqCost c(s, G, rows);
-    it.P = c.P;
+    it.P = (int)c.P;
     const int64_t head = c.sum(c.items);
     int64_t rest = x - before;
     it.kv = 0;
@@ -150,7 +150,7 @@ struct Items {
       const int64_t m = (i + j) / 2;
       if (c.sum(m) <= rest) i = m; else j = m;
     }
-    it.p0 = i * rows;
+    it.p0 = __builtin_amdgcn_readfirstlane((int)i * rows);
     it.start = before + it.kv * head + c.sum(i);
     it.end = before + it.kv * head + c.sum(i + 1);
     return it;
@@ -168,32 +168,72 @@ struct Items {
 };
 
 // A unit's walk over its items: body(item, lo, hi, whole, slot) for each, with the keys
-// [lo, hi) of it that are the unit's.
-template <typename F>
+// [lo, hi) of it that are the unit's.  Between items the walk's own state waits in
+// LDS, a copy a wave, so that it takes no registers from the body.
+struct Walk {
+  Item it;
+  int64_t lo, hi;
+};
+template <int WAVES, typename F>
 __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&body) {
+  __shared__ Walk state[WAVES];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items items(a);
-  const int G = items.G, step = a.plan.step;
-  const int64_t N = items.total();
-  int64_t q = (N + a.plan.units - 1) / a.plan.units;
-  q = scalar64(max(q, (int64_t)step * G));
-  const int64_t lo = unit * q, hi = min(lo + q, N);
   PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
-  if (lo < hi) {
-    Item it = items.find(lo);
-    if (it.start < lo && it.start >= lo - q)    // this unit holds the item's first cut
-      cut = PageCut{unit - 1, (int)((it.end - 1) / q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, 0, it.p0, it.P};
-    for (int slot = 0;; slot = 1) {
+  bool any;
+  {
+    const int64_t N = items.total();
+    int64_t q = (N + a.plan.units - 1) / a.plan.units;
+    q = scalar64(max(q, (int64_t)a.plan.step * items.G));
+    const int64_t lo = unit * q, hi = min(lo + q, N);
+    any = lo < hi;
+    if (any) {
+      const Item it = items.find(lo);
+      if (it.start < lo && it.start >= lo - q)    // this unit holds the item's first cut
+        cut = PageCut{unit - 1, (int)((it.end - 1) / q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, it.p0, it.P, 0};
+      state[wave] = Walk{it, lo, hi};
+    }
+    if (a.plan.units > 1 && threadIdx.x == 0) a.cuts[unit] = cut;
+  }
+  if (!any) return;
+  for (int slot = 0;; slot = 1) {
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    {
+      const Walk &w = state[wave];
+      Item it;
+      it.b = __builtin_amdgcn_readfirstlane(w.it.b);
+      it.kv = __builtin_amdgcn_readfirstlane(w.it.kv);
+      it.p0 = __builtin_amdgcn_readfirstlane(w.it.p0);
+      it.P = __builtin_amdgcn_readfirstlane(w.it.P);
+      it.seq.r0 = __builtin_amdgcn_readfirstlane(w.it.seq.r0);
+      it.seq.n = __builtin_amdgcn_readfirstlane(w.it.seq.n);
+      it.seq.len = __builtin_amdgcn_readfirstlane(w.it.seq.len);
       // the keys its last row sees
-      const int last = (int)((min(it.p0 + a.plan.rows, it.P) - 1) / G);
+      const int last = (min(it.p0 + a.plan.rows, it.P) - 1) / items.G;
       const int end = max(0, it.seq.len - it.seq.n + last + 1);
-      auto key_at = [&](int64_t x) { return (int)min((x - it.start) / G / step * step, (int64_t)end); };
-      const int k0 = it.start >= lo ? 0 : key_at(lo), k1 = it.end <= hi ? end : key_at(hi);
-      body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), it.start >= lo && it.end <= hi, slot);
-      if (it.end >= hi) break;
-      it = items.next(it);
+      auto key_at = [&](int64_t x) {
+        return (int)min((x - w.it.start) / items.G / a.plan.step * a.plan.step, (int64_t)end);
+      };
+      const bool head = w.it.start >= w.lo, tail = w.it.end <= w.hi;
+      const int k0 = head ? 0 : key_at(w.lo), k1 = tail ? end : key_at(w.hi);
+      body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1),
+           __builtin_amdgcn_readfirstlane(head && tail ? 1 : 0) != 0, slot);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    {
+      Item it = state[wave].it;
+      it.start = scalar64(it.start);
+      it.end = scalar64(it.end);
+      if (it.end >= scalar64(state[wave].hi)) return;
+      it.b = __builtin_amdgcn_readfirstlane(it.b);
+      it.kv = __builtin_amdgcn_readfirstlane(it.kv);
+      it.p0 = __builtin_amdgcn_readfirstlane(it.p0);
+      it.seq.r0 = __builtin_amdgcn_readfirstlane(it.seq.r0);
+      it.seq.n = __builtin_amdgcn_readfirstlane(it.seq.n);
+      it.seq.len = __builtin_amdgcn_readfirstlane(it.seq.len);
+      state[wave].it = items.next(it);
     }
   }
-  if (a.plan.units > 1 && threadIdx.x == 0) a.cuts[unit] = cut;
 }
 
 // Workgroups are dispatched to the 8 XCDs round-robin; consecutive units, which read
@@ -265,20 +305,20 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
   __shared__ __attribute__((aligned(16))) float so[NW][16][D + 4];
   __shared__ float2 sml[NW][16];
 
-  walk_items(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
+  walk_items<NW>(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
     // keys [lo, hi); row i of the sequence sees those below base + i + 1
     const PageSeq seq = it.seq;
     const int kv = it.kv;
-    const int64_t p0 = it.p0, P = it.P;
-    const int first = (int)(p0 / G), base = seq.len - seq.n;
+    const int p0 = it.p0, P = it.P;
+    const int first = __builtin_amdgcn_readfirstlane(p0 / G), base = seq.len - seq.n;
     const int32_t *table = a.seqs.tables + (int64_t)it.b * a.seqs.max_pages;
 
     bf16x8 qf[RT][KK];
     int vis[RT];                            // keys this lane's row sees
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int64_t p = p0 + 16 * t + n16;
-      const int i = p < P ? (int)(p / G) : 0, g = p < P ? (int)(p - (int64_t)i * G) : 0;
+      const int p = p0 + 16 * t + n16;
+      const int i = p < P ? p / G : 0, g = p < P ? p - i * G : 0;
       vis[t] = p < P ? base + i + 1 : 0;
       const uint16_t *q = a.q + (int64_t)(seq.r0 + i) * a.q_stride + (int64_t)(kv * G + g) * D;
 #pragma unroll
@@ -493,7 +533,7 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
       }
       __syncthreads();
       const int row = threadIdx.x / 16, piece = threadIdx.x % 16;   // (PC channels)
-      const int64_t p = p0 + 16 * t + row;
+      const int p = p0 + 16 * t + row;
       if (p >= P) continue;
       float m = sml[0][row].x;
 #pragma unroll
@@ -508,7 +548,7 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
 #pragma unroll
         for (int i = 0; i < PC; ++i) acc[i] += e * so[w][row][PC * piece + i];
       }
-      const int i = (int)(p / G), g = (int)(p - (int64_t)i * G);
+      const int i = p / G, g = p - i * G;
       const int64_t at = (int64_t)(seq.r0 + i) * Hq + kv * G + g;
       if (!whole) {
         const int64_t at2 = (int64_t)(2 * unit + slot) * (16 * RT) + 16 * t + row;
@@ -594,24 +634,24 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
   const int tr_row = 4 * half + ((lane & 15) >> 2);
   const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 
-  walk_items(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
+  walk_items<MW>(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
     const PageSeq seq = it.seq;
     const int kv = it.kv;
-    const int64_t p0 = it.p0, P = it.P;
-    const int first = (int)(p0 / G), base = seq.len - seq.n;
+    const int p0 = it.p0, P = it.P;
+    const int first = __builtin_amdgcn_readfirstlane(p0 / G), base = seq.len - seq.n;
     const int all_see = base + first + 1;   // keys that every row of the item sees
     const int32_t *table = a.seqs.tables + (int64_t)it.b * a.seqs.max_pages;
     const uint8_t *blocks = pool.pages + (int64_t)kv * pool.block_bytes;
 
     // this lane's query row
-    const int64_t p = p0 + 32 * wave + l32;
+    const int p = p0 + 32 * wave + l32;
     const bool row_ok = p < P;
     const bool wave_rows = p0 + 32 * wave < P;    // (a wave without rows still fetches)
-    const int r = row_ok ? (int)(p / G) : 0, g = row_ok ? (int)(p - (int64_t)r * G) : 0;
-    const int vis = row_ok ? base + r + 1 : 0;    // keys it sees
-    const int64_t at = (int64_t)(seq.r0 + r) * Hq + kv * G + g;
+    int vis;                                // keys it sees
     bf16x8 qf[D / 16];
     {
+      const int r = row_ok ? p / G : 0, g = row_ok ? p - r * G : 0;
+      vis = row_ok ? base + r + 1 : 0;
       const uint16_t *q = a.q + (int64_t)(seq.r0 + r) * a.q_stride + (int64_t)(kv * G + g) * D + 8 * half;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) qf[kk] = row_ok ? *reinterpret_cast<const bf16x8 *>(q + 16 * kk) : bf16x8{};
@@ -801,13 +841,13 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
       load(t + 2);
       if (wave_rows) compute(1, t + 1, Open{});
     }
+    // (the rest are masked, needed or not: with both kinds in this loop the kernel takes
+    // 345 registers instead of 202, and spills)
     for (int b = 0; t < t_hi; ++t, b ^= 1) {
       store_tile(b);
       __syncthreads();
       if (t + 1 < t_hi) load(t + 1);
-      if (!wave_rows) continue;
-      if ((t + 1) * MK > all_see) compute(b, t, Masked{});
-      else compute(b, t, Open{});
+      if (wave_rows) compute(b, t, Masked{});
     }
 
     const float l = l_run + __shfl_xor(l_run, 32);
@@ -821,6 +861,8 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
           op[i * 64] = float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
       }
     } else if (row_ok) {
+      const int r = p / G;
+      const int64_t at = (int64_t)(seq.r0 + r) * Hq + kv * G + (p - r * G);
       const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row sees nothing; a NaN stays one)
 #pragma unroll
       for (int i = 0; i < D / 8; ++i)
@@ -912,8 +954,7 @@ __global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
     t.w += e * y.w;
   }
   const int G = a.pool.Hq / a.pool.Hkv;
-  const int64_t p = cut.p0 + row;
-  const int r = (int)(p / G), g = (int)(p - (int64_t)r * G);
+  const int p = cut.p0 + row, r = p / G, g = p - r * G;
   const int64_t at = (int64_t)(cut.r0 + r) * a.pool.Hq + cut.kv * G + g;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   *reinterpret_cast<uint2 *>(a.out + at * D + ch) =

@@ -27,6 +27,7 @@ int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
   if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
   if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
   if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;
+  if ((int64_t)b->n_rows * (p->n_q_heads / p->n_kv_heads) > 1 << 30) return HERMES_EINVAL;
   // the cost of all items of an attention call has to fit 62 bits (items of 16 rows, one more a pair)
   const double G = (double)p->n_q_heads / p->n_kv_heads, keys = (double)b->max_pages * p->page_rows;
   const double items = (double)b->n_rows * p->n_q_heads / 16.0 + (double)b->n_seqs * p->n_kv_heads;

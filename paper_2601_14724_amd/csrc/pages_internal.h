@@ -65,8 +65,8 @@ struct PageCut {
   int32_t first, last;      // units (last < first: no item is first cut here)
   int32_t slot;             // of the first unit's part: 0 or 1 (the others: 0)
   int32_t kv, r0;           // KV head, first stacked row of the sequence
+  int32_t p0, P;            // the item's first packed row, the sequence's packed rows
   int32_t pad_;
-  int64_t p0, P;            // the item's first packed row, the sequence's packed rows
 };
 
 struct PageAttnArgs {
