@@ -74,13 +74,35 @@ struct SeqCost {
   }
 };
 
-__device__ __forceinline__ int64_t shfl64(int64_t x, int lane) {
-  const uint32_t lo = __shfl((int)(uint32_t)x, lane), hi = __shfl((int)(x >> 32), lane);
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
+__device__ __forceinline__ int64_t pair64(uint32_t lo, uint32_t hi) { return (int64_t)((uint64_t)hi << 32 | lo); }
 __device__ __forceinline__ int64_t scalar64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
+  return pair64(__builtin_amdgcn_readfirstlane((int)(uint32_t)x), __builtin_amdgcn_readfirstlane((int)(x >> 32)));
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int lane) {
+  return pair64(__builtin_amdgcn_readlane((int)(uint32_t)x, lane), __builtin_amdgcn_readlane((int)(x >> 32), lane));
+}
+// x of the lane that a data-parallel move names, 0 where it names none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved64(int64_t x) {
+  return pair64(__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xF, false),
+                __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xF, false));
+}
+// inclusive sums over the lanes: within rows of 16 by shifts of 1, 2, 4 and 8, then the
+// last lane of row 0 to row 1 and of 2 to 3, then lane 31 to rows 2 and 3
+__device__ __forceinline__ int64_t wave_sums(int64_t x) {
+  x += moved64<0x111, 0xF>(x);
+  x += moved64<0x112, 0xF>(x);
+  x += moved64<0x114, 0xF>(x);
+  x += moved64<0x118, 0xF>(x);
+  x += moved64<0x142, 0xA>(x);
+  x += moved64<0x143, 0xC>(x);
+  return x;
+}
+// x / y of scalars, 0 <= x, 0 < y (64-bit divisions are some 100 instructions, and the
+// start of a short call waits for them)
+__device__ __forceinline__ int64_t over64(int64_t x, int64_t y) {
+  if (((x | y) >> 32) == 0) return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)x / (uint32_t)y));
+  return scalar64((int64_t)((uint64_t)x / (uint64_t)y));
 }
 
 // The items of a call, a sequence a lane.
@@ -98,32 +120,30 @@ struct Items {
       const SeqCost c(page_seq(pool, seqs, b0 + lane), G, rows);
       x = pool.Hkv * c.sum(c.items);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = shfl64(x, max(lane - o, 0));
-      if (lane >= o) x += y;
-    }
-    return x;
+    return wave_sums(x);
   }
-  __device__ __forceinline__ int64_t total() const {
-    int64_t n = 0;
-    for (int b = 0; b < seqs.n_seqs; b += 64) n += scalar64(shfl64(scan(b), 63));
+  // the cost of all, and scan(0)
+  __device__ __forceinline__ int64_t total(int64_t *sums) const {
+    *sums = scan(0);
+    int64_t n = lane64(*sums, 63);
+    for (int b = 64; b < seqs.n_seqs; b += 64) n += lane64(scan(b), 63);
     return n;
   }
-  // The item that holds x (x < total).
-  __device__ __forceinline__ Item find(int64_t x) const {
+  // The item that holds x (x < total); sums: scan(0).
+  __device__ __forceinline__ Item find(int64_t x, int64_t sums) const {
     int64_t before = 0;
     int b = 0;
-    for (;; b += 64) {
-      const int64_t sums = scan(b);
+    for (;;) {
       const unsigned long long past = __ballot(before + sums > x);
       if (past != 0ull || b + 64 >= seqs.n_seqs) {
         const int l = past != 0ull ? __builtin_ctzll(past) : 63;
-        before += l > 0 ? scalar64(shfl64(sums, l - 1)) : 0;
+        before += l > 0 ? lane64(sums, l - 1) : 0;
         b += l;
         break;
       }
-      before += scalar64(shfl64(sums, 63));
+      before += lane64(sums, 63);
+      b += 64;
+      sums = scan(b);
     }
     return in_sequence(b, before, x);
   }
@@ -142,7 +162,7 @@ struct Items {
     int64_t rest = x - before;
     it.kv = 0;
     if (pool.Hkv > 1) {
-      it.kv = (int)scalar64(rest / head);
+      it.kv = (int)over64(rest, head);
       rest -= it.kv * head;
     }
     int64_t i = 0, j = c.items;           // sum(i) <= rest < sum(j)
@@ -179,23 +199,34 @@ __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&
   __shared__ Walk state[WAVES];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items items(a);
-  PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
-  bool any;
-  {
-    const int64_t N = items.total();
-    int64_t q = (N + a.plan.units - 1) / a.plan.units;
-    q = scalar64(max(q, (int64_t)a.plan.step * items.G));
+  const int tiles = a.plan.tiles;           // > 0: no cuts, `tiles` units for each pair
+  if (tiles > 0) {
+    Walk w;
+    const int pair = unit / tiles;
+    w.it.b = pair / a.pool.Hkv;
+    w.it.kv = pair - w.it.b * a.pool.Hkv;
+    w.it.seq = page_seq(a.pool, a.seqs, w.it.b);
+    w.it.P = w.it.seq.n * items.G;
+    w.it.p0 = (unit - pair * tiles) * a.plan.rows;
+    w.it.start = w.lo = 0;
+    w.it.end = w.hi = 1;
+    if (w.it.p0 >= w.it.P) return;
+    state[wave] = w;
+  } else {
+    PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
+    int64_t sums;
+    const int64_t N = items.total(&sums);
+    const int64_t q = max(over64(N + a.plan.units - 1, a.plan.units), (int64_t)a.plan.step * items.G);
     const int64_t lo = unit * q, hi = min(lo + q, N);
-    any = lo < hi;
-    if (any) {
-      const Item it = items.find(lo);
+    if (lo < hi) {
+      const Item it = items.find(lo, sums);
       if (it.start < lo && it.start >= lo - q)    // this unit holds the item's first cut
-        cut = PageCut{unit - 1, (int)((it.end - 1) / q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, it.p0, it.P, 0};
+        cut = PageCut{unit - 1, (int)over64(it.end - 1, q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, it.p0, it.P, 0};
       state[wave] = Walk{it, lo, hi};
     }
-    if (a.plan.units > 1 && threadIdx.x == 0) a.cuts[unit] = cut;
+    if (threadIdx.x == 0) a.cuts[unit] = cut;
+    if (lo >= hi) return;
   }
-  if (!any) return;
   for (int slot = 0;; slot = 1) {
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     {
@@ -208,26 +239,33 @@ __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&
       it.seq.r0 = __builtin_amdgcn_readfirstlane(w.it.seq.r0);
       it.seq.n = __builtin_amdgcn_readfirstlane(w.it.seq.n);
       it.seq.len = __builtin_amdgcn_readfirstlane(w.it.seq.len);
+      const int64_t start = scalar64(w.it.start), lo = scalar64(w.lo), hi = scalar64(w.hi);
       // the keys its last row sees
       const int last = (min(it.p0 + a.plan.rows, it.P) - 1) / items.G;
       const int end = max(0, it.seq.len - it.seq.n + last + 1);
       auto key_at = [&](int64_t x) {
-        return (int)min((x - w.it.start) / items.G / a.plan.step * a.plan.step, (int64_t)end);
+        const int64_t keys = over64(x - start, items.G);
+        return (int)min(keys & -(int64_t)a.plan.step, (int64_t)end);   // (a step is a power of two)
       };
-      const bool head = w.it.start >= w.lo, tail = w.it.end <= w.hi;
-      const int k0 = head ? 0 : key_at(w.lo), k1 = tail ? end : key_at(w.hi);
-      body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1),
-           __builtin_amdgcn_readfirstlane(head && tail ? 1 : 0) != 0, slot);
+      const bool head = start >= lo, tail = scalar64(w.it.end) <= hi;
+      const int k0 = head ? 0 : key_at(lo), k1 = tail ? end : key_at(hi);
+      body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), head && tail, slot);
     }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     {
       Item it = state[wave].it;
       it.start = scalar64(it.start);
       it.end = scalar64(it.end);
+      it.p0 = __builtin_amdgcn_readfirstlane(it.p0);
+      if (tiles > 0) {                      // (more rows than the hint said)
+        const int64_t p0 = it.p0 + (int64_t)tiles * a.plan.rows;
+        if (p0 >= __builtin_amdgcn_readfirstlane(it.P)) return;
+        state[wave].it.p0 = (int)p0;
+        continue;
+      }
       if (it.end >= scalar64(state[wave].hi)) return;
       it.b = __builtin_amdgcn_readfirstlane(it.b);
       it.kv = __builtin_amdgcn_readfirstlane(it.kv);
-      it.p0 = __builtin_amdgcn_readfirstlane(it.p0);
       it.seq.r0 = __builtin_amdgcn_readfirstlane(it.seq.r0);
       it.seq.n = __builtin_amdgcn_readfirstlane(it.seq.n);
       it.seq.len = __builtin_amdgcn_readfirstlane(it.seq.len);
@@ -288,6 +326,7 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
   using B = PageBlock<D, FP4>;
   constexpr int KK = D / 32;                // MFMAs of S for each group of keys
   constexpr int PC = D / 16;                // channels of a piece of V
+  constexpr int AHEAD = FP4 ? 2 : 1;        // steps in flight beside the one computed
   const PagePool &pool = a.pool;
   const int Hq = pool.Hq, G = Hq / pool.Hkv;
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
@@ -377,12 +416,12 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
         }
       }
     };
-    auto compute = [&](Frag &f, int x, auto masked) {
+    auto step = [&](Frag &f, int x) {
       const int key0 = key_of(x);
-      if constexpr (decltype(masked)::value) {
-        // Memory that holds no stored row (past the length, or no page) may hold
-        // anything: its values become zeros.  Keys there are masked by S, or
-        // zeros too.
+      // Memory that holds no stored row (past the length, or no page) may hold
+      // anything: its values become zeros.  Keys there are masked by S, or zeros too.
+      const bool hole = (__builtin_amdgcn_readlane(ids[0], x & 63) | __builtin_amdgcn_readlane(ids[1], x & 63)) < 0;
+      if (__builtin_expect(hole || key0 + KS > seq.len, 0)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const bool none = __builtin_amdgcn_readlane(ids[h], x & 63) < 0;
@@ -395,19 +434,15 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
               if constexpr (D == 128) f.v[h][j] = 0u;
               else f.v[h][j / 2] &= j & 1 ? 0x0000FFFFu : 0xFFFF0000u;
             }
-            if (none) {
-              f.ks[h] = 0u;
-#pragma unroll
-              for (int i = 0; i < Frag::WK; ++i) f.k[h][i] = 0u;
-            }
+            if (none) f.ks[h] = 0u;
           } else {
 #pragma unroll
             for (int i = 0; i < Frag::WV; ++i)
               if (i / (Frag::WV / 4) >= valid) f.v[h][i] = 0u;
-            if (none) {
+          }
+          if (none) {
 #pragma unroll
-              for (int i = 0; i < Frag::WK; ++i) f.k[h][i] = 0u;
-            }
+            for (int i = 0; i < Frag::WK; ++i) f.k[h][i] = 0u;
           }
         }
       }
@@ -427,17 +462,17 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
           for (int t = 0; t < RT; ++t) s[t][h] = mfma16(kf, qf[t][kk], s[t][h]);
         }
       }
+      if (key0 + KS > all_see) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (key0 + 16 * (j / 4) + 4 * u + j % 4 >= vis[t]) s[t][j / 4][j % 4] = -INFINITY;
+        }
+      }
       bf16x8 pf[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        if constexpr (decltype(masked)::value) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (key0 + 16 * h + 4 * u + j >= vis[t]) s[t][h][j] = -INFINITY;
-          }
-        }
         float mx = s[t][0][0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[t][j / 4][j % 4]);
@@ -496,22 +531,20 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
         }
       }
     };
-    using Masked = std::integral_constant<bool, true>;
-    using Open = std::integral_constant<bool, false>;
-    auto step = [&](Frag &f, int x) {
-      const bool hole = (__builtin_amdgcn_readlane(ids[0], x & 63) | __builtin_amdgcn_readlane(ids[1], x & 63)) < 0;
-      if (hole || key_of(x) + KS > all_see) compute(f, x, Masked{});
-      else compute(f, x, Open{});
-    };
+    // a ring of steps in registers, AHEAD of them in flight
     for (int x0 = 0; x0 < mine; x0 += 64) {
       find_pages(x0);
-      const int n = min(64, mine - x0);
-      Frag cur, nxt;
-      load(cur, x0);
-      for (int x = x0; x < x0 + n; ++x) {
-        if (x + 1 < x0 + n) load(nxt, x + 1);
-        step(cur, x);
-        cur = nxt;
+      const int x1 = min(x0 + 64, mine);
+      Frag f[AHEAD + 1];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (x0 + i < x1) load(f[i], x0 + i);
+      for (int x = x0; x < x1; x += AHEAD + 1) {
+#pragma unroll
+        for (int i = 0; i <= AHEAD; ++i) {
+          if (x + i + AHEAD < x1) load(f[(i + AHEAD) % (AHEAD + 1)], x + i + AHEAD);
+          if (x + i < x1) step(f[i], x + i);
+        }
       }
     }
 
@@ -970,7 +1003,7 @@ hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   else if (rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2>), grid, dim3(NT), 0, s, a);
   else hipLaunchKernelGGL((page_attn_many<D, FP4>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.plan.units == 1) return e;
+  if (e != hipSuccess || a.plan.tiles > 0) return e;
   const dim3 joins(a.plan.units, rows * D / 256);
   if (rows <= 64) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);

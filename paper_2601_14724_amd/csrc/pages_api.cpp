@@ -62,18 +62,26 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   PagePlan x;
   x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 256;
   x.step = x.rows <= 64 ? 128 : 64;
-  // no more units than steps, nor than fit the CUs (two workgroups of four waves, or
-  // one of eight)
-  const int64_t steps = (int64_t)b->n_seqs * p->n_kv_heads * over(P, x.rows) * over(max_len, x.step);
+  // The slots: two workgroups of four waves a CU, or one of eight.  Without cuts a launch
+  // takes rounds of items, with cuts its steps are shared out, at the price of a
+  // second launch.
   const int64_t slots = x.rows <= 64 ? 2 * kStreamSlots : kStreamSlots;
-  x.units = (int32_t)(steps < slots ? steps : slots);
+  const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles, steps = over(max_len, x.step);
+  const int64_t spare = over(items, slots) * steps - over(items * steps, slots);
+  if (spare <= (x.rows <= 64 ? 8 : 4) && items <= 1 << 24) {
+    x.tiles = (int32_t)tiles;
+    x.units = (int32_t)items;
+  } else {
+    x.tiles = 0;
+    x.units = (int32_t)(items * steps < slots ? items * steps : slots);
+  }
   return x;
 }
 
 // Workspace: the cuts, then O and (max, sum) of 2 units parts.
 size_t cuts_bytes(const PagePlan &x) { return (sizeof(PageCut) * (size_t)x.units + 255) / 256 * 256; }
 size_t workspace_of(const hermes_page_pool *p, const PagePlan &x) {
-  if (x.units == 1) return 0;
+  if (x.tiles > 0) return 0;
   return cuts_bytes(x) + sizeof(float) * 2 * (size_t)x.units * x.rows * (p->head_dim + 2);
 }
 

@@ -54,9 +54,11 @@ struct PagePackArgs {
 // head of the KV head) of one (sequence, KV head), against all keys its rows see.
 // The items, in order, are cut into `units` runs of equal cost, a workgroup each, at
 // least `step` keys long: the lengths are on the device, so the kernel finds its run.
+// Where cuts would save less than they cost, there are none (`tiles` > 0): every pair
+// has `tiles` units, each for a tile (for more, if the pair has more tiles than that).
 // rows up to 64 take page_attn_few, more page_attn_many.
 struct PagePlan {
-  int32_t rows, units, step;
+  int32_t rows, units, step, tiles;
 };
 
 // What page_combine has to know of a cut item, written by the unit that holds its
