@@ -909,90 +909,143 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 
 // -------------------------------------------------------------------- the joins
 // O = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m) over the parts s of a cut
-// item.  Workgroup (u, y): item that unit u cut first, 64 float4 of its O; wave w
-// takes the parts w, w + 4, ..., four loaded at once, and the waves' sums are joined
-// in wave order.
+// item.  A task is 256 float4 of an item of a few parts, 64 a wave, or 64 of an item of
+// more, whose parts its four waves share out (wave w takes w, w + 4, ..., and their sums
+// are joined in wave order); its loads are four parts at once.  Most units hold no
+// first cut when items are long, so every workgroup adds up all cuts' tasks and takes
+// every gridDim.x-th (with a workgroup for each (unit, 64 float4), 64 rows on 8192 tokens
+// took 34 us here, most of it workgroups that found nothing to do).
+constexpr int kJoinUnits = 512;         // units of a launch at most
+constexpr int kFewParts = 4;
+
 template <int D, bool MANY>
 __global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
-  const PageCut cut = a.cuts[blockIdx.x];
-  if (cut.last < cut.first) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  // which row and channels float4 `i` of a part holds
-  const int i = blockIdx.y * 64 + lane;
-  int row, ch;
-  if constexpr (MANY) {     // [32 rows][channels / 8][lane]
-    row = i / (D / 8 * 64) * 32 + i % 32;
-    ch = i / 64 % (D / 8) * 8 + i / 32 % 2 * 4;
-  } else {
-    row = i / (D / 4);
-    ch = i % (D / 4) * 4;
-  }
-  const int rows = a.plan.rows;
-  if (__all(cut.p0 + row >= cut.P)) return;
-  const int parts = cut.last - cut.first + 1;
-  auto part = [&](int s) { return (int64_t)2 * (cut.first + s) + (s == 0 ? cut.slot : 0); };
-  float m = kLowest, l = 0.f;
-  float4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int AHEAD = 4;
-  for (int s0 = wave; s0 < parts; s0 += 4 * AHEAD) {
-    float2 ml[AHEAD];
-    float4 o[AHEAD];
-#pragma unroll
-    for (int x = 0; x < AHEAD; ++x) {
-      const int s = s0 + 4 * x;
-      ml[x] = float2{kLowest, 0.f};
-      o[x] = float4{0.f, 0.f, 0.f, 0.f};
-      if (s < parts && cut.p0 + row < cut.P) {
-        ml[x] = *reinterpret_cast<const float2 *>(a.mlpart + 2 * (part(s) * rows + row));
-        o[x] = reinterpret_cast<const float4 *>(a.opart + part(s) * rows * D)[i];
-      }
-    }
-    float mn = m;
-#pragma unroll
-    for (int x = 0; x < AHEAD; ++x) mn = fmaxf(mn, ml[x].x);
-    const float old = fast_exp2(m - mn);
-    m = mn;
-    l *= old;
-    acc = float4{acc.x * old, acc.y * old, acc.z * old, acc.w * old};
-#pragma unroll
-    for (int x = 0; x < AHEAD; ++x) {
-      if (ml[x].y == 0.f) continue;        // (an empty part, whose O was not written)
-      const float w = fast_exp2(ml[x].x - m);
-      l += w * ml[x].y;
-      acc.x += w * o[x].x;
-      acc.y += w * o[x].y;
-      acc.z += w * o[x].z;
-      acc.w += w * o[x].w;
-    }
-  }
+  __shared__ int upto[kJoinUnits];      // tasks of the cuts 0 .. i
+  __shared__ int wsum[4];
   __shared__ float4 sacc[4][64];
   __shared__ float2 sml[4][64];
-  sacc[wave][lane] = acc;
-  sml[wave][lane] = float2{m, l};
-  __syncthreads();
-  if (wave != 0 || cut.p0 + row >= cut.P) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int rows = a.plan.rows;
+  // float4 groups of 64 that hold rows of a cut's item
+  auto groups = [&](const PageCut &c) {
+    const int n = min(rows, c.P - c.p0);
+    return MANY ? (n + 31) / 32 * (D / 8) : (n * (D / 4) + 63) / 64;
+  };
+  // thread t has the cuts 2 t and 2 t + 1
+  int n[2];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) m = fmaxf(m, sml[w][lane].x);
-  float4 t = {0.f, 0.f, 0.f, 0.f};
-  l = 0.f;
+  for (int x = 0; x < 2; ++x) {
+    const int i = 2 * threadIdx.x + x;
+    n[x] = 0;
+    if (i < a.plan.units) {
+      const PageCut c = a.cuts[i];
+      const int parts = c.last - c.first + 1;
+      if (parts > 0) n[x] = parts > kFewParts ? groups(c) : (groups(c) + 3) / 4;
+    }
+  }
+  const int64_t sums = wave_sums(n[0] + n[1]);
+  if (lane == 63) wsum[wave] = (int)sums;
+  __syncthreads();
+  int before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const float2 x = sml[w][lane];
-    const float4 y = sacc[w][lane];
-    const float e = fast_exp2(x.x - m);
-    l += e * x.y;
-    t.x += e * y.x;
-    t.y += e * y.y;
-    t.z += e * y.z;
-    t.w += e * y.w;
+    before += w < wave ? wsum[w] : 0;
+    total += wsum[w];
   }
-  const int G = a.pool.Hq / a.pool.Hkv;
-  const int p = cut.p0 + row, r = p / G, g = p - r * G;
-  const int64_t at = (int64_t)(cut.r0 + r) * a.pool.Hq + cut.kv * G + g;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  *reinterpret_cast<uint2 *>(a.out + at * D + ch) =
-      uint2{f2bf(t.x * inv) | f2bf(t.y * inv) << 16, f2bf(t.z * inv) | f2bf(t.w * inv) << 16};
-  if (a.lse != nullptr && ch == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  upto[2 * threadIdx.x + 1] = before + (int)sums;
+  upto[2 * threadIdx.x] = before + (int)sums - n[1];
+  __syncthreads();
+
+  for (int task = blockIdx.x; task < total; task += gridDim.x) {
+    int lo = 0, hi = kJoinUnits - 1;    // the first cut with upto > task
+    while (lo < hi) {
+      const int m = (lo + hi) / 2;
+      if (upto[m] > task) hi = m; else lo = m + 1;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const PageCut cut = a.cuts[lo];
+    const int parts = cut.last - cut.first + 1, nth = task - (lo > 0 ? upto[lo - 1] : 0);
+    const bool shared = parts > kFewParts;
+    // which row and channels float4 `i` of a part holds
+    const int i = (shared ? nth : 4 * nth + wave) * 64 + lane;
+    int row, ch;
+    if constexpr (MANY) {     // [32 rows][channels / 8][lane]
+      row = i / (D / 8 * 64) * 32 + i % 32;
+      ch = i / 64 % (D / 8) * 8 + i / 32 % 2 * 4;
+    } else {
+      row = i / (D / 4);
+      ch = i % (D / 4) * 4;
+    }
+    const bool ok = row < min(rows, cut.P - cut.p0);
+    auto part = [&](int s) { return (int64_t)2 * (cut.first + s) + (s == 0 ? cut.slot : 0); };
+    float m = kLowest, l = 0.f;
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int AHEAD = 4;
+    const int step = shared ? 4 : 1;
+    for (int s0 = shared ? wave : 0; s0 < parts; s0 += step * AHEAD) {
+      float2 ml[AHEAD];
+      float4 o[AHEAD];
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) {
+        const int s = s0 + step * x;
+        ml[x] = float2{kLowest, 0.f};
+        o[x] = float4{0.f, 0.f, 0.f, 0.f};
+        if (s < parts && ok) {
+          ml[x] = *reinterpret_cast<const float2 *>(a.mlpart + 2 * (part(s) * rows + row));
+          o[x] = reinterpret_cast<const float4 *>(a.opart + part(s) * rows * D)[i];
+        }
+      }
+      float mn = m;
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) mn = fmaxf(mn, ml[x].x);
+      const float old = fast_exp2(m - mn);
+      m = mn;
+      l *= old;
+      acc = float4{acc.x * old, acc.y * old, acc.z * old, acc.w * old};
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) {
+        if (ml[x].y == 0.f) continue;      // (an empty part, whose O was not written)
+        const float w = fast_exp2(ml[x].x - m);
+        l += w * ml[x].y;
+        acc.x += w * o[x].x;
+        acc.y += w * o[x].y;
+        acc.z += w * o[x].z;
+        acc.w += w * o[x].w;
+      }
+    }
+    if (shared) {
+      sacc[wave][lane] = acc;
+      sml[wave][lane] = float2{m, l};
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) m = fmaxf(m, sml[w][lane].x);
+        acc = float4{0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float2 x = sml[w][lane];
+          const float4 y = sacc[w][lane];
+          const float e = fast_exp2(x.x - m);
+          l += e * x.y;
+          acc.x += e * y.x;
+          acc.y += e * y.y;
+          acc.z += e * y.z;
+          acc.w += e * y.w;
+        }
+      }
+      __syncthreads();                     // (the next task writes there)
+      if (wave != 0) continue;
+    }
+    if (!ok) continue;
+    const int G = a.pool.Hq / a.pool.Hkv;
+    const int p = cut.p0 + row, r = p / G, g = p - r * G;
+    const int64_t at = (int64_t)(cut.r0 + r) * a.pool.Hq + cut.kv * G + g;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint2 *>(a.out + at * D + ch) =
+        uint2{f2bf(acc.x * inv) | f2bf(acc.y * inv) << 16, f2bf(acc.z * inv) | f2bf(acc.w * inv) << 16};
+    if (a.lse != nullptr && ch == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
 }
 
 template <int D, bool FP4>
@@ -1004,7 +1057,7 @@ hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   else hipLaunchKernelGGL((page_attn_many<D, FP4>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan.tiles > 0) return e;
-  const dim3 joins(a.plan.units, rows * D / 256);
+  const dim3 joins(2 * kJoinUnits);
   if (rows <= 64) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);
   return hipGetLastError();
