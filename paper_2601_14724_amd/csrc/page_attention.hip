@@ -11,7 +11,7 @@
 // every workgroup (unit) adds up the items' costs and takes an equal run of them,
 // [u q, (u + 1) q) of N with q = ceil(N / units).  The cost of item i of a
 // (sequence, KV head) pair is, in 1/G keys, G max(T - n, 0) + min((i + 1) rows, n G)
-// + kItemKeys G: the keys its last row sees, and a constant for its start and end.
+// + item_keys G: the keys its last row sees, and a constant for its start and end.
 // That is an arithmetic progression, so the sums over a sequence's items, and the
 // item that holds a point, need no loop over items.  A cut inside an item falls on a
 // multiple of the step.  Items that lie in one unit are written at once; of a cut
@@ -27,7 +27,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NT = 256, NW = NT / 64;
+constexpr int NT = 512, NW = NT / 64;
 constexpr int KS = 32;                  // keys of a wave's step (page_attn_few)
 constexpr float kLowest = -3.0e38f;     // running maximum before the first key (finite: -inf minus it stays -inf)
 constexpr float kLn2 = 0.69314718055994531f;
@@ -50,8 +50,6 @@ __device__ __forceinline__ uint32_t fp4_pair(uint32_t codes, float scale, int by
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // ---------------------------------------------------------------------- the cut
-constexpr int kItemKeys = 128;          // what an item's start and end cost, in keys
-
 struct Item {
   PageSeq seq;
   int b, kv;
@@ -62,10 +60,10 @@ struct Item {
 // A sequence's costs: sum(i) of its first i items a KV head.
 struct SeqCost {
   int64_t base, P, rows, items;
-  __device__ __forceinline__ SeqCost(const PageSeq &s, int G, int rows_) {
-    base = (int64_t)G * (max(s.len - s.n, 0) + kItemKeys);
+  __device__ __forceinline__ SeqCost(const PageSeq &s, int G, const PagePlan &plan) {
+    base = (int64_t)G * (max(s.len - s.n, 0) + plan.item_keys);
     P = (int64_t)s.n * G;
-    rows = rows_;
+    rows = plan.rows;
     items = (P + rows - 1) / rows;
   }
   __device__ __forceinline__ int64_t sum(int64_t i) const {
@@ -109,81 +107,91 @@ __device__ __forceinline__ int64_t over64(int64_t x, int64_t y) {
 struct Items {
   const PagePool &pool;
   const PageSeqs &seqs;
-  int rows, G;
+  const PagePlan &plan;
+  int G;
   __device__ __forceinline__ Items(const PageAttnArgs &a)
-      : pool(a.pool), seqs(a.seqs), rows(a.plan.rows), G(a.pool.Hq / a.pool.Hkv) {}
-  // inclusive sums of the costs of sequences b0 ..
-  __device__ __forceinline__ int64_t scan(int b0) const {
+      : pool(a.pool), seqs(a.seqs), plan(a.plan), G(a.pool.Hq / a.pool.Hkv) {}
+  // Lane l has sequence b0 + l: its bounds, and the sum of the costs up to it.
+  struct Scan {
+    PageSeq seq;
+    int64_t sums;
+  };
+  __device__ __forceinline__ Scan scan(int b0) const {
     const int lane = threadIdx.x & 63;
-    int64_t x = 0;
+    Scan x = {{0, 0, 0}, 0};
     if (b0 + lane < seqs.n_seqs) {
-      const SeqCost c(page_seq(pool, seqs, b0 + lane), G, rows);
-      x = pool.Hkv * c.sum(c.items);
+      x.seq = page_seq(pool, seqs, b0 + lane);
+      const SeqCost c(x.seq, G, plan);
+      x.sums = pool.Hkv * c.sum(c.items);
     }
-    return wave_sums(x);
+    x.sums = wave_sums(x.sums);
+    return x;
   }
-  // the cost of all, and scan(0)
-  __device__ __forceinline__ int64_t total(int64_t *sums) const {
-    *sums = scan(0);
-    int64_t n = lane64(*sums, 63);
-    for (int b = 64; b < seqs.n_seqs; b += 64) n += lane64(scan(b), 63);
+  // the cost of all; first: scan(0)
+  __device__ __forceinline__ int64_t total(const Scan &first) const {
+    int64_t n = lane64(first.sums, 63);
+    for (int b = 64; b < seqs.n_seqs; b += 64) n += lane64(scan(b).sums, 63);
     return n;
   }
-  // The item that holds x (x < total); sums: scan(0).
-  __device__ __forceinline__ Item find(int64_t x, int64_t sums) const {
+  // The item that holds x (x < total); s: scan(0).
+  __device__ __forceinline__ Item find(int64_t x, Scan s) const {
     int64_t before = 0;
-    int b = 0;
+    int b = 0, l;
     for (;;) {
-      const unsigned long long past = __ballot(before + sums > x);
-      if (past != 0ull || b + 64 >= seqs.n_seqs) {
-        const int l = past != 0ull ? __builtin_ctzll(past) : 63;
-        before += l > 0 ? lane64(sums, l - 1) : 0;
-        b += l;
-        break;
-      }
-      before += lane64(sums, 63);
+      const unsigned long long past = __ballot(before + s.sums > x);
+      l = past != 0ull ? __builtin_ctzll(past) : 63;
+      if (past != 0ull || b + 64 >= seqs.n_seqs) break;
+      before += lane64(s.sums, 63);
       b += 64;
-      sums = scan(b);
+      s = scan(b);
     }
-    return in_sequence(b, before, x);
+    before += l > 0 ? lane64(s.sums, l - 1) : 0;
+    const PageSeq seq = {__builtin_amdgcn_readlane(s.seq.r0, l), __builtin_amdgcn_readlane(s.seq.n, l),
+                         __builtin_amdgcn_readlane(s.seq.len, l)};
+    return in_sequence(b + l, seq, before, x);
+  }
+  __device__ __forceinline__ PageSeq sequence(int b) const {
+    const PageSeq s = page_seq(pool, seqs, b);
+    return {__builtin_amdgcn_readfirstlane(s.r0), __builtin_amdgcn_readfirstlane(s.n),
+            __builtin_amdgcn_readfirstlane(s.len)};
   }
   // The item that holds x, in sequence b, whose items start at `before`.
-  __device__ __forceinline__ Item in_sequence(int b, int64_t before, int64_t x) const {
+  __device__ __forceinline__ Item in_sequence(int b, const PageSeq &seq, int64_t before, int64_t x) const {
     Item it;
     it.b = b;
-    PageSeq s = page_seq(pool, seqs, b);
-    s.r0 = __builtin_amdgcn_readfirstlane(s.r0);
-    s.n = __builtin_amdgcn_readfirstlane(s.n);
-    s.len = __builtin_amdgcn_readfirstlane(s.len);
-    it.seq = s;
-    const SeqCost c(s, G, rows);
+    it.seq = seq;
+    const SeqCost c(seq, G, plan);
     it.P = (int)c.P;
     const int64_t head = c.sum(c.items);
     int64_t rest = x - before;
-    it.kv = 0;
-    if (pool.Hkv > 1) {
+    if (pool.Hkv <= 64) {                 // (a lane a head, for a division)
+      const int lane = threadIdx.x & 63;
+      const unsigned long long past = __ballot(lane + 1 >= pool.Hkv || (lane + 1) * head > rest);
+      it.kv = __builtin_ctzll(past);
+    } else {
       it.kv = (int)over64(rest, head);
-      rest -= it.kv * head;
     }
+    rest -= it.kv * head;
     int64_t i = 0, j = c.items;           // sum(i) <= rest < sum(j)
     while (j - i > 1) {
       const int64_t m = (i + j) / 2;
       if (c.sum(m) <= rest) i = m; else j = m;
     }
-    it.p0 = __builtin_amdgcn_readfirstlane((int)i * rows);
+    it.p0 = __builtin_amdgcn_readfirstlane((int)i * plan.rows);
     it.start = before + it.kv * head + c.sum(i);
     it.end = before + it.kv * head + c.sum(i + 1);
     return it;
   }
   // The item after `it`, if any (it.end < total).
   __device__ __forceinline__ Item next(const Item &it) const {
-    const SeqCost c(it.seq, G, rows);
+    const SeqCost c(it.seq, G, plan);
     const int64_t all = pool.Hkv * c.sum(c.items), head = c.sum(c.items);
-    const int64_t before = it.start - it.kv * head - c.sum(it.p0 / rows);
-    if (it.end < before + all) return in_sequence(it.b, before, it.end);
+    const int64_t before = it.start - it.kv * head - c.sum(it.p0 / plan.rows);
+    if (it.end < before + all) return in_sequence(it.b, it.seq, before, it.end);
     int b = it.b + 1;                      // (sequences without rows have no items)
-    while (b + 1 < seqs.n_seqs && __builtin_amdgcn_readfirstlane(page_seq(pool, seqs, b).n) == 0) ++b;
-    return in_sequence(b, it.end, it.end);
+    PageSeq seq = sequence(b);
+    while (b + 1 < seqs.n_seqs && seq.n == 0) seq = sequence(++b);
+    return in_sequence(b, seq, it.end, it.end);
   }
 };
 
@@ -214,17 +222,18 @@ __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&
     state[wave] = w;
   } else {
     PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
-    int64_t sums;
-    const int64_t N = items.total(&sums);
-    const int64_t q = max(over64(N + a.plan.units - 1, a.plan.units), (int64_t)a.plan.step * items.G);
+    const Items::Scan first = items.scan(0);
+    const int64_t N = items.total(first);
+    const int64_t q = max((int64_t)((double)N * a.plan.inv_units) + 1, (int64_t)a.plan.step * items.G);
     const int64_t lo = unit * q, hi = min(lo + q, N);
     if (lo < hi) {
-      const Item it = items.find(lo, sums);
-      if (it.start < lo && it.start >= lo - q)    // this unit holds the item's first cut
+      const Item it = items.find(lo, first);
+      // (the wave with the fewest steps) this unit holds the item's first cut
+      if (wave == WAVES - 1 && it.start < lo && it.start >= lo - q)
         cut = PageCut{unit - 1, (int)over64(it.end - 1, q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, it.p0, it.P, 0};
       state[wave] = Walk{it, lo, hi};
     }
-    if (threadIdx.x == 0) a.cuts[unit] = cut;
+    if (threadIdx.x == 64 * WAVES - 1) a.cuts[unit] = cut;
     if (lo >= hi) return;
   }
   for (int slot = 0;; slot = 1) {
@@ -244,7 +253,7 @@ __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&
       const int last = (min(it.p0 + a.plan.rows, it.P) - 1) / items.G;
       const int end = max(0, it.seq.len - it.seq.n + last + 1);
       auto key_at = [&](int64_t x) {
-        const int64_t keys = over64(x - start, items.G);
+        const int64_t keys = (int64_t)((double)(x - start) * a.plan.inv_group);
         return (int)min(keys & -(int64_t)a.plan.step, (int64_t)end);   // (a step is a power of two)
       };
       const bool head = start >= lo, tail = scalar64(w.it.end) <= hi;
@@ -322,7 +331,7 @@ __device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *p) {
 }
 
 template <int D, bool FP4, int RT>
-__global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArgs a) {
+__global__ __launch_bounds__(NT, 1) void page_attn_few(PageAttnArgs a) {
   using B = PageBlock<D, FP4>;
   constexpr int KK = D / 32;                // MFMAs of S for each group of keys
   constexpr int PC = D / 16;                // channels of a piece of V
@@ -341,8 +350,10 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
   const int ks_ofs = B::ks(page_rows, n16) + u * (D / 4) / 32;
   const int vs_ofs = B::vs(page_rows, u) + n16 * PC / 32 * 4;
 
-  __shared__ __attribute__((aligned(16))) float so[NW][16][D + 4];
-  __shared__ float2 sml[NW][16];
+  // the waves' states, in two buffers: a wave may leave its next one while others still read
+  __shared__ __attribute__((aligned(16))) float so_[2][NW][16][D + 4];
+  __shared__ float2 sml_[2][NW][16];
+  int joins = 0;
 
   walk_items<NW>(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
     // keys [lo, hi); row i of the sequence sees those below base + i + 1
@@ -548,14 +559,16 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
       }
     }
 
-    // join the waves' states, 16 rows at a time: thread (row, piece of eight channels)
+    // join the waves' states, 16 rows at a time
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (p0 + 16 * t >= P) break;
       float l = l_run[t];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      __syncthreads();
+      float(*so)[16][D + 4] = so_[joins & 1];
+      float2(*sml)[16] = sml_[joins & 1];
+      ++joins;
       if (u == 0) sml[wave][n16] = float2{m_run[t], l};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -565,43 +578,41 @@ __global__ __launch_bounds__(NT, RT == 1 ? 2 : 1) void page_attn_few(PageAttnArg
               float4{o[t][i][j], o[t][i + 1][j], o[t][i + 2][j], o[t][i + 3][j]};
       }
       __syncthreads();
-      const int row = threadIdx.x / 16, piece = threadIdx.x % 16;   // (PC channels)
+      constexpr int TPR = NT / 16, CPT = D / TPR;                    // threads of a row, channels of a thread
+      const int row = threadIdx.x / TPR, ch = threadIdx.x % TPR * CPT;
       const int p = p0 + 16 * t + row;
       if (p >= P) continue;
       float m = sml[0][row].x;
 #pragma unroll
       for (int w = 1; w < NW; ++w) m = fmaxf(m, sml[w][row].x);
-      float sum = 0.f, acc[PC];
+      float sum = 0.f, acc[CPT];
 #pragma unroll
-      for (int i = 0; i < PC; ++i) acc[i] = 0.f;
+      for (int i = 0; i < CPT; ++i) acc[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         const float e = fast_exp2(sml[w][row].x - m);
         sum += e * sml[w][row].y;
 #pragma unroll
-        for (int i = 0; i < PC; ++i) acc[i] += e * so[w][row][PC * piece + i];
+        for (int i = 0; i < CPT; ++i) acc[i] += e * so[w][row][ch + i];
       }
-      const int i = p / G, g = p - i * G;
-      const int64_t at = (int64_t)(seq.r0 + i) * Hq + kv * G + g;
       if (!whole) {
-        const int64_t at2 = (int64_t)(2 * unit + slot) * (16 * RT) + 16 * t + row;
-        if (piece == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * at2) = float2{m, sum};
+        const int64_t at = (int64_t)(2 * unit + slot) * (16 * RT) + 16 * t + row;
+        if (ch == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * at) = float2{m, sum};
         if (hi > lo) {                      // (an empty part leaves its O unwritten, and unread)
 #pragma unroll
-          for (int x = 0; x < PC; x += 4)
-            *reinterpret_cast<float4 *>(a.opart + at2 * D + PC * piece + x) =
-                float4{acc[x], acc[x + 1], acc[x + 2], acc[x + 3]};
+          for (int x = 0; x < CPT; x += 2)
+            *reinterpret_cast<float2 *>(a.opart + at * D + ch + x) = float2{acc[x], acc[x + 1]};
         }
       } else {
+        const int i = p / G, g = p - i * G;
+        const int64_t at = (int64_t)(seq.r0 + i) * Hq + kv * G + g;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (0: the row sees nothing; a NaN stays one)
 #pragma unroll
-        for (int x = 0; x < PC; x += 4)
-          *reinterpret_cast<uint2 *>(a.out + at * D + PC * piece + x) =
-              uint2{f2bf(acc[x] * inv) | f2bf(acc[x + 1] * inv) << 16, f2bf(acc[x + 2] * inv) | f2bf(acc[x + 3] * inv) << 16};
-        if (a.lse != nullptr && piece == 0) a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
+        for (int x = 0; x < CPT; x += 2)
+          *reinterpret_cast<uint32_t *>(a.out + at * D + ch + x) = f2bf(acc[x] * inv) | f2bf(acc[x + 1] * inv) << 16;
+        if (a.lse != nullptr && ch == 0) a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
       }
     }
-    __syncthreads();   // so and sml are free for the next item
   });
 }
 

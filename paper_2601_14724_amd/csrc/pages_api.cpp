@@ -61,11 +61,11 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t P = max_rows * G;
   PagePlan x;
   x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 256;
-  x.step = x.rows <= 64 ? 128 : 64;
-  // The slots: two workgroups of four waves a CU, or one of eight.  Without cuts a launch
-  // takes rounds of items, with cuts its steps are shared out, at the price of a
-  // second launch.
-  const int64_t slots = x.rows <= 64 ? 2 * kStreamSlots : kStreamSlots;
+  x.item_keys = x.rows > 64 ? 320 : p->format == HERMES_PAGE_FP4 ? 1024 : 512;
+  x.step = x.rows <= 64 ? 256 : 64;
+  // A workgroup of eight waves fits a CU.  Without cuts a launch takes rounds of items,
+  // with cuts its steps are shared out, at the price of a second launch.
+  const int64_t slots = kStreamSlots;
   const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles, steps = over(max_len, x.step);
   const int64_t spare = over(items, slots) * steps - over(items * steps, slots);
   if (spare <= (x.rows <= 64 ? 8 : 4) && items <= 1 << 24) {
@@ -75,6 +75,8 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
     x.tiles = 0;
     x.units = (int32_t)(items * steps < slots ? items * steps : slots);
   }
+  x.inv_units = 1.0 / x.units;
+  x.inv_group = 1.0 / (double)G;
   return x;
 }
 

@@ -59,6 +59,8 @@ struct PagePackArgs {
 // rows up to 64 take page_attn_few, more page_attn_many.
 struct PagePlan {
   int32_t rows, units, step, tiles;
+  int32_t item_keys;        // what an item's start and end cost, in keys
+  double inv_units, inv_group;   // 1 / units, 1 / (query heads of a KV head)
 };
 
 // What page_combine has to know of a cut item, written by the unit that holds its
