@@ -1,7 +1,7 @@
 // Causal attention over pages for gfx950 (MFMA bf16, 64-wide waves).
 //
 // page_attn_few    up to 32 packed rows (row, query head of the KV head) an item
-// page_attn_many   256 packed rows an item
+// page_attn_many   64, 128 or 256 packed rows an item
 // page_combine     joins the parts of items that were cut
 //
 // S = scale q k^T over the keys a row sees, O = softmax(S) V, in one pass over the
@@ -621,15 +621,15 @@ __global__ __launch_bounds__(NT, 1) void page_attn_few(PageAttnArgs a) {
 // .. + 7] and B[k = 8 (l / 32) .. + 7][n = l % 32]; result register j of lane l holds
 // D[m = 8 (j / 4) + 4 (l / 32) + j % 4][n = l % 32].
 //
-// Eight waves of 32 packed rows share every tile of 64 keys: each wave fetches eight
-// keys' K and V from the page (so a page id is a scalar, and a KV head's 4 bits cost
-// a workgroup 8.5 KB a tile), turns FP4 into bf16 on the way to LDS, and all read
-// the tile from there, K row by row and V transposed by ds_read_b64_tr_b16.  As in
-// attn_fwd, S^T = K Q^T puts one query row a lane, so the softmax stays in the lane and
-// P^T is the B operand of O^T = V^T P^T as it is.
+// Eight waves: RG row groups of 32 packed rows, times KG = 8 / RG key groups, each of
+// which takes every KG-th tile of keys and holds all the item's rows, so that items of
+// 64 or 128 rows keep the matrix units as busy as those of 256; the key groups' states are
+// merged through LDS at an item's end.  A wave fetches its share of its group's tile from
+// the page (8 or 16 keys, so a page id is a scalar), turns FP4 into bf16 on the way to LDS,
+// and reads all of the tile from there, K row by row and V transposed by
+// ds_read_b64_tr_b16.  As in attn_fwd, S^T = K Q^T puts one query row a lane, so the softmax
+// stays in the lane and P^T is the B operand of O^T = V^T P^T as it is.
 constexpr int MT = 512, MW = MT / 64;   // waves
-constexpr int MROWS = 32 * MW;          // packed rows of an item
-constexpr int MK = 64;                  // keys of a tile
 constexpr int KPAD = 8, VPAD = 32;      // u16 padding of K and V rows in LDS
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -644,15 +644,19 @@ __device__ __forceinline__ s4 lds_tr16(const uint16_t *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
 }
 
-template <int D, bool FP4>
+template <int D, bool FP4, int RG>
 __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
   using B = PageBlock<D, FP4>;
-  constexpr int WKEYS = MK / MW;          // keys a wave fetches
+  constexpr int KG = MW / RG, MROWS = 32 * RG;   // key groups, packed rows of an item
+  constexpr int MK = KG <= 2 ? 64 : 32;   // keys of a tile (four groups' tiles of 64 do not fit LDS)
+  constexpr int SUB = MK / 32;
+  constexpr int WKEYS = MK / RG;          // keys a wave fetches
+  static_assert(WKEYS == 8 || WKEYS == 16, "a wave's keys lie in one page");
   constexpr int UK = WKEYS * D / 8 / 64;  // pieces of eight channels of K a lane fetches
   constexpr int LK = D / 8 / UK;          // lanes of a key
-  constexpr int PC = D / 16;              // channels of a piece of V; a lane fetches one of two keys
-  static_assert(WKEYS / 4 * 16 * 2 == 64, "two keys' piece of V a lane");
-  constexpr int WK = FP4 ? UK : 4 * UK, WV = FP4 ? D / 64 : D / 16;   // words a lane fetches
+  constexpr int PC = D / 16;              // channels of a piece of V; a lane fetches one of two keys,
+  constexpr int NV = WKEYS / 8;           // NV times, eight keys apart
+  constexpr int WK = FP4 ? UK : 4 * UK, WV = FP4 ? D / 64 : D / 16;   // words a lane fetches (of V NV times)
   constexpr int kAheadK = 4, kAheadV = 4; // LDS reads issued ahead of their MFMA
 
   const PagePool &pool = a.pool;
@@ -660,11 +664,12 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int half = lane >> 5, l32 = lane & 31;
+  const int rg = wave % RG, kg = wave / RG;
   const int rows_log = pool.log_rows, page_rows = 1 << rows_log;
   const float c = a.scale_log2, inv_c = 1.f / c;
 
-  // what this lane fetches: of key `kkey` of the wave's eight, channels 8 kpc ..; of keys
-  // vkey and vkey + 1, channels PC vpc ..
+  // what this lane fetches: of key `kkey` of the wave's, channels 8 kpc ..; of keys vkey and
+  // vkey + 1 (and eight further), channels PC vpc ..
   const int kkey = lane / LK, kpc = lane % LK * UK;
   const int vpc = lane % 32 / 2, vkey = lane / 32 * 4 + lane % 2 * 2;
   const int k_ofs = B::k(kkey) + kpc * (FP4 ? 4 : 16);
@@ -672,8 +677,10 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
   const int ks_ofs = B::ks(page_rows, kkey) + kpc * 8 / 32;
   const int vs_ofs = B::vs(page_rows, lane / 32) + vpc * PC / 32 * 4 + lane % 2 * 2;
 
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[2][MK][D + KPAD];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[2][MK][D + VPAD];
+  // two tiles of K and V for each key group
+  __shared__ __attribute__((aligned(16))) uint16_t tiles[KG * 2 * MK * (D + KPAD + D + VPAD)];
+  uint16_t(*Ks)[MK][D + KPAD] = reinterpret_cast<uint16_t(*)[MK][D + KPAD]>(tiles) + 2 * kg;
+  uint16_t(*Vs)[MK][D + VPAD] = reinterpret_cast<uint16_t(*)[MK][D + VPAD]>(tiles + KG * 2 * MK * (D + KPAD)) + 2 * kg;
   // transposed-read coordinates of this lane inside its 16-lane group
   const int tr_row = 4 * half + ((lane & 15) >> 2);
   const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -688,9 +695,9 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
     const uint8_t *blocks = pool.pages + (int64_t)kv * pool.block_bytes;
 
     // this lane's query row
-    const int p = p0 + 32 * wave + l32;
+    const int p = p0 + 32 * rg + l32;
     const bool row_ok = p < P;
-    const bool wave_rows = p0 + 32 * wave < P;    // (a wave without rows still fetches)
+    const bool wave_rows = p0 + 32 * rg < P;      // (a wave without rows still fetches)
     int vis;                                // keys it sees
     bf16x8 qf[D / 16];
     {
@@ -706,14 +713,17 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
     float m_run = kLowest, l_run = 0.f;
     float m_lim = (kLowest + 8.f) * inv_c;
 
-    // lane x holds the page of this wave's keys of tile t0 + x (-1: none)
+    // Step s: tiles t_lo + s KG .. + KG - 1, one for each key group.  Lane x holds the page
+    // of this wave's keys of step ids_at + x (-1: none)
     const int t_hi = (hi + MK - 1) / MK, t_lo = lo < hi ? lo / MK : t_hi;   // (an empty part starts anywhere)
-    int ids = -1, ids_at = t_lo;
-    auto find_pages = [&](int t) {
-      ids_at = t;
-      const int64_t key = (int64_t)(t + lane) * MK + wave * WKEYS;
+    const int steps = (t_hi - t_lo + KG - 1) / KG;
+    auto tile = [&](int s) { return t_lo + s * KG + kg; };
+    int ids = -1, ids_at = 0;
+    auto find_pages = [&](int s) {
+      ids_at = s;
+      const int64_t key = (int64_t)tile(s + lane) * MK + rg * WKEYS;
       ids = -1;
-      if (t + lane < t_hi && key < hi) {
+      if (s + lane < steps && key < hi) {
         ids = table[key >> rows_log];
         if (ids < 0 || ids >= pool.n_pages) {
           ids = -1;
@@ -721,17 +731,22 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
         }
       }
     };
-    uint32_t kw[WK], vw[WV], ksc = 0, vsc = 0;
-    auto load = [&](int t) {
-      if (t - ids_at >= 64) find_pages(t);
-      const int id = __builtin_amdgcn_readlane(ids, t - ids_at);
-      const int key0 = t * MK + wave * WKEYS, row = key0 & (page_rows - 1);
+    uint32_t kw[WK], vw[NV][WV], ksc = 0, vsc[NV];
+#pragma unroll
+    for (int z = 0; z < NV; ++z) vsc[z] = 0;
+    auto load = [&](int s) {
+      if (s - ids_at >= 64) find_pages(s);
+      const int id = __builtin_amdgcn_readlane(ids, s - ids_at);
+      const int key0 = tile(s) * MK + rg * WKEYS, row = key0 & (page_rows - 1);
       const uint8_t *block = blocks + (int64_t)max(id, 0) * pool.page_bytes;
       load_words<WK>(kw, block + row * B::kRow + k_ofs);
-      load_words<WV>(vw, block + row * B::kRow + v_ofs);
+#pragma unroll
+      for (int z = 0; z < NV; ++z) load_words<WV>(vw[z], block + (row + 8 * z) * B::kRow + v_ofs);
       if constexpr (FP4) {
         ksc = *(block + row * B::kScales + ks_ofs);
-        vsc = *reinterpret_cast<const uint16_t *>(block + row * B::kScales + vs_ofs);
+#pragma unroll
+        for (int z = 0; z < NV; ++z)
+          vsc[z] = *reinterpret_cast<const uint16_t *>(block + (row + 8 * z) * B::kScales + vs_ofs);
       }
       // what lies past the length, or in no page, may be anything: zeros instead
       if (__builtin_expect(id < 0 || key0 + WKEYS > seq.len, 0)) {
@@ -742,21 +757,24 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
           for (int i = 0; i < WK; ++i) kw[i] = 0u;
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (vkey + j < valid) continue;
-          if constexpr (FP4) {
-            vsc &= ~(0xFFu << (8 * j));
-            if constexpr (D == 128) vw[j] = 0u;
-            else vw[0] &= j == 1 ? 0x0000FFFFu : 0xFFFF0000u;
-          } else {
+        for (int z = 0; z < NV; ++z) {
 #pragma unroll
-            for (int i = 0; i < WV / 2; ++i) vw[j * (WV / 2) + i] = 0u;
+          for (int j = 0; j < 2; ++j) {
+            if (vkey + 8 * z + j < valid) continue;
+            if constexpr (FP4) {
+              vsc[z] &= ~(0xFFu << (8 * j));
+              if constexpr (D == 128) vw[z][j] = 0u;
+              else vw[z][0] &= j == 1 ? 0x0000FFFFu : 0xFFFF0000u;
+            } else {
+#pragma unroll
+              for (int i = 0; i < WV / 2; ++i) vw[z][j * (WV / 2) + i] = 0u;
+            }
           }
         }
       }
     };
     auto store_tile = [&](int b) {
-      uint16_t *kd = &Ks[b][wave * WKEYS + kkey][kpc * 8];
+      uint16_t *kd = &Ks[b][rg * WKEYS + kkey][kpc * 8];
       const float sc = scale_of(ksc);
 #pragma unroll
       for (int i = 0; i < UK; ++i) {
@@ -766,26 +784,30 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
         *reinterpret_cast<uint4 *>(kd + 8 * i) = x;
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint16_t *vd = &Vs[b][wave * WKEYS + vkey + j][vpc * PC];
-        const float vs = scale_of(j == 0 ? vsc & 0xFFu : vsc >> 8);
-        if constexpr (D == 128) {
-          uint4 x;
-          if constexpr (FP4) x = uint4{fp4_pair(vw[j], vs, 0), fp4_pair(vw[j], vs, 1), fp4_pair(vw[j], vs, 2), fp4_pair(vw[j], vs, 3)};
-          else x = uint4{vw[4 * j], vw[4 * j + 1], vw[4 * j + 2], vw[4 * j + 3]};
-          *reinterpret_cast<uint4 *>(vd) = x;
-        } else {
-          uint2 x;
-          if constexpr (FP4) x = uint2{fp4_pair(vw[0], vs, 2 * j), fp4_pair(vw[0], vs, 2 * j + 1)};
-          else x = uint2{vw[2 * j], vw[2 * j + 1]};
-          *reinterpret_cast<uint2 *>(vd) = x;
+      for (int z = 0; z < NV; ++z) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint16_t *vd = &Vs[b][rg * WKEYS + vkey + 8 * z + j][vpc * PC];
+          const uint32_t *w = vw[z];
+          const float vs = scale_of(j == 0 ? vsc[z] & 0xFFu : vsc[z] >> 8);
+          if constexpr (D == 128) {
+            uint4 x;
+            if constexpr (FP4) x = uint4{fp4_pair(w[j], vs, 0), fp4_pair(w[j], vs, 1), fp4_pair(w[j], vs, 2), fp4_pair(w[j], vs, 3)};
+            else x = uint4{w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]};
+            *reinterpret_cast<uint4 *>(vd) = x;
+          } else {
+            uint2 x;
+            if constexpr (FP4) x = uint2{fp4_pair(w[0], vs, 2 * j), fp4_pair(w[0], vs, 2 * j + 1)};
+            else x = uint2{w[2 * j], w[2 * j + 1]};
+            *reinterpret_cast<uint2 *>(vd) = x;
+          }
         }
       }
     };
     auto compute = [&](int b, int t, auto masked) {
-      f32x16 s[2];
+      f32x16 s[SUB];
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
+      for (int sub = 0; sub < SUB; ++sub) {
         s[sub] = f32x16{};
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
@@ -794,7 +816,7 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < kAheadK; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
-      for (int i = 0; i < 2 * (D / 16) - kAheadK; ++i) {
+      for (int i = 0; i < SUB * (D / 16) - kAheadK; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
@@ -802,7 +824,7 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
       for (int i = 0; i < kAheadK; ++i) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       if constexpr (decltype(masked)::value) {
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
+        for (int sub = 0; sub < SUB; ++sub) {
 #pragma unroll
           for (int jj = 0; jj < 16; ++jj)
             if (t * MK + sub * 32 + 8 * (jj >> 2) + 4 * half + (jj & 3) >= vis) s[sub][jj] = -INFINITY;
@@ -810,7 +832,7 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
+      for (int sub = 0; sub < SUB; ++sub) {
 #pragma unroll
         for (int jj = 0; jj < 16; ++jj) mx = fmaxf(mx, s[sub][jj]);
       }
@@ -830,10 +852,10 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
       }
-      bf16x8 pf[4];
+      bf16x8 pf[2 * SUB];
       float ls = 0.f;
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
+      for (int sub = 0; sub < SUB; ++sub) {
 #pragma unroll
         for (int jj = 0; jj < 16; ++jj) {
           const float x = fast_exp2(fmaf(s[sub][jj], c, -m_run));
@@ -846,13 +868,13 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
 #pragma unroll
-        for (int qq = 0; qq < 4; ++qq) {
+        for (int qq = 0; qq < 2 * SUB; ++qq) {
           const uint16_t *vp = &Vs[b][16 * qq + tr_row][32 * db + tr_col];
           const s4 x = lds_tr16(vp), y = lds_tr16(vp + 8 * (D + VPAD));
           o[db] = mfma32(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7)), pf[qq], o[db]);
         }
       }
-      constexpr int kPV = D / 32 * 4;
+      constexpr int kPV = D / 32 * 2 * SUB;
 #pragma unroll
       for (int i = 0; i < 2 * kAheadV; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
 #pragma unroll
@@ -867,53 +889,101 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 
     using Masked = std::integral_constant<bool, true>;
     using Open = std::integral_constant<bool, false>;
-    __syncthreads();                        // the tiles of the item before are read
-    if (t_lo < t_hi) {
-      find_pages(t_lo);
-      load(t_lo);
+    __syncthreads();                        // the tiles (or states) of the item before are read
+    if (steps > 0) {
+      find_pages(0);
+      load(0);
     }
-    // tiles that every row sees whole, two a trip so that each LDS buffer is a constant
-    const int t_open = min(t_hi - 1, all_see / MK);
-    int t = t_lo;
-    for (; t + 1 < t_open; t += 2) {
+    // steps whose tiles every row sees whole, two a trip so that each LDS buffer is a constant
+    const int s_open = min(steps - 1, all_see > t_lo * MK ? (all_see / MK - t_lo) / KG : 0);
+    int s = 0;
+    for (; s + 1 < s_open; s += 2) {
       store_tile(0);
       __syncthreads();
-      load(t + 1);
-      if (wave_rows) compute(0, t, Open{});
+      load(s + 1);
+      if (wave_rows) compute(0, tile(s), Open{});
       store_tile(1);
       __syncthreads();
-      load(t + 2);
-      if (wave_rows) compute(1, t + 1, Open{});
+      load(s + 2);
+      if (wave_rows) compute(1, tile(s + 1), Open{});
     }
     // (the rest are masked, needed or not: with both kinds in this loop the kernel takes
     // 345 registers instead of 202, and spills)
-    for (int b = 0; t < t_hi; ++t, b ^= 1) {
+    for (int b = 0; s < steps; ++s, b ^= 1) {
       store_tile(b);
       __syncthreads();
-      if (t + 1 < t_hi) load(t + 1);
-      if (wave_rows) compute(b, t, Masked{});
+      if (s + 1 < steps) load(s + 1);
+      if (wave_rows && (KG == 1 || tile(s) < t_hi)) compute(b, tile(s), Masked{});
     }
 
-    const float l = l_run + __shfl_xor(l_run, 32);
-    if (row_ok && !whole) {
-      const int64_t part = (int64_t)(2 * unit + slot) * MROWS + 32 * wave;
-      if (half == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * (part + l32)) = float2{m_run, l};
-      float4 *op = reinterpret_cast<float4 *>(a.opart + part * D) + lane;   // [channels / 8][lane]
-      if (hi > lo) {
+    // The key groups' states merge through LDS: every wave leaves its (max, sum) and O there,
+    // then wave kg of a row group merges the KG-th part of the channels, groups in order.
+    // fn(c, x) gets channels 8 c + 4 half .. of this lane's row.
+    constexpr int NC = D / 8;
+    float l = l_run + __shfl_xor(l_run, 32);
+    auto own = [&](int i) {
+      return float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    };
+    auto merge = [&](auto fn) {
+      if constexpr (KG == 1) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-          op[i * 64] = float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+        for (int i = 0; i < NC; ++i) fn(i, own(i));
+      } else {
+        static_assert(MW * NC * 64 * 16 + MW * 32 * 8 <= (int)sizeof(tiles), "the states fit");
+        float4 *mo = reinterpret_cast<float4 *>(tiles);
+        float2 *mm = reinterpret_cast<float2 *>(mo + MW * NC * 64);
+        __syncthreads();                    // all tiles are read
+#pragma unroll
+        for (int i = 0; i < NC; ++i) mo[(wave * NC + i) * 64 + lane] = own(i);
+        if (half == 0) mm[wave * 32 + l32] = float2{m_run, l};
+        __syncthreads();
+        float w[KG];
+        m_run = kLowest;
+#pragma unroll
+        for (int x = 0; x < KG; ++x) m_run = fmaxf(m_run, mm[(x * RG + rg) * 32 + l32].x);
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < KG; ++x) {
+          const float2 y = mm[(x * RG + rg) * 32 + l32];
+          w[x] = fast_exp2(y.x - m_run);
+          l += w[x] * y.y;
+        }
+#pragma unroll
+        for (int i = 0; i < NC / KG; ++i) {
+          const int at = kg * (NC / KG) + i;
+          float4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < KG; ++x) {
+            const float4 y = mo[((x * RG + rg) * NC + at) * 64 + lane];
+            t.x += w[x] * y.x;
+            t.y += w[x] * y.y;
+            t.z += w[x] * y.z;
+            t.w += w[x] * y.w;
+          }
+          fn(at, t);
+        }
       }
-    } else if (row_ok) {
-      const int r = p / G;
-      const int64_t at = (int64_t)(seq.r0 + r) * Hq + kv * G + (p - r * G);
-      const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row sees nothing; a NaN stays one)
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i)
-        *reinterpret_cast<uint2 *>(a.out + at * D + 8 * i + 4 * half) =
-            uint2{f2bf(o[i / 4][4 * (i % 4)] * inv) | f2bf(o[i / 4][4 * (i % 4) + 1] * inv) << 16,
-                  f2bf(o[i / 4][4 * (i % 4) + 2] * inv) | f2bf(o[i / 4][4 * (i % 4) + 3] * inv) << 16};
-      if (a.lse != nullptr && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
+    };
+    if (!whole) {
+      const int64_t part = (int64_t)(2 * unit + slot) * MROWS + 32 * rg;
+      float4 *op = reinterpret_cast<float4 *>(a.opart + part * D) + lane;   // [channels / 8][lane]
+      if (hi > lo) {                        // (an empty part leaves its O unwritten, and unread)
+        merge([&](int i, float4 x) {
+          if (row_ok) op[i * 64] = x;
+        });
+      }
+      if (row_ok && half == 0 && kg == 0) *reinterpret_cast<float2 *>(a.mlpart + 2 * (part + l32)) = float2{m_run, l};
+    } else {
+      const int r = row_ok ? p / G : 0;
+      const int64_t at = (int64_t)(seq.r0 + r) * Hq + kv * G + (row_ok ? p - r * G : 0);
+      uint16_t *orow = a.out + at * D + 4 * half;
+      merge([&](int i, float4 x) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row sees nothing; a NaN stays one)
+        if (row_ok)
+          *reinterpret_cast<uint2 *>(orow + 8 * i) =
+              uint2{f2bf(x.x * inv) | f2bf(x.y * inv) << 16, f2bf(x.z * inv) | f2bf(x.w * inv) << 16};
+      });
+      if (row_ok && a.lse != nullptr && half == 0 && kg == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
     }
   });
 }
@@ -1065,11 +1135,13 @@ hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   const int rows = a.plan.rows;
   if (rows == 16) hipLaunchKernelGGL((page_attn_few<D, FP4, 1>), grid, dim3(NT), 0, s, a);
   else if (rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2>), grid, dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL((page_attn_many<D, FP4>), grid, dim3(MT), 0, s, a);
+  else if (rows == 64) hipLaunchKernelGGL((page_attn_many<D, FP4, 2>), grid, dim3(MT), 0, s, a);
+  else if (rows == 128) hipLaunchKernelGGL((page_attn_many<D, FP4, 4>), grid, dim3(MT), 0, s, a);
+  else hipLaunchKernelGGL((page_attn_many<D, FP4, 8>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan.tiles > 0) return e;
   const dim3 joins(2 * kJoinUnits);
-  if (rows <= 64) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
+  if (rows <= 32) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);
   return hipGetLastError();
 }

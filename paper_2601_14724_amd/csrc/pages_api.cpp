@@ -60,15 +60,15 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t max_len = b->max_len > 0 && b->max_len < table ? b->max_len : table;
   const int64_t P = max_rows * G;
   PagePlan x;
-  x.rows = P <= 16 ? 16 : P <= 32 ? 32 : 256;
-  x.item_keys = x.rows > 64 ? 320 : p->format == HERMES_PAGE_FP4 ? 1024 : 512;
-  x.step = x.rows <= 64 ? 256 : 64;
+  x.rows = P <= 16 ? 16 : P <= 32 ? 32 : P <= 64 ? 64 : P <= 128 ? 128 : 256;
+  x.item_keys = x.rows > 32 ? 320 : p->format == HERMES_PAGE_FP4 ? 1024 : 512;
+  x.step = x.rows <= 32 ? 256 : x.rows <= 128 ? 128 : 64;   // (a step of all a workgroup's key groups)
   // A workgroup of eight waves fits a CU.  Without cuts a launch takes rounds of items,
   // with cuts its steps are shared out, at the price of a second launch.
   const int64_t slots = kStreamSlots;
   const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles, steps = over(max_len, x.step);
   const int64_t spare = over(items, slots) * steps - over(items * steps, slots);
-  if (spare <= (x.rows <= 64 ? 8 : 4) && items <= 1 << 24) {
+  if (spare <= (x.rows <= 32 ? 8 : 4) && items <= 1 << 24) {
     x.tiles = (int32_t)tiles;
     x.units = (int32_t)items;
   } else {

@@ -56,7 +56,7 @@ struct PagePackArgs {
 // least `step` keys long: the lengths are on the device, so the kernel finds its run.
 // Where cuts would save less than they cost, there are none (`tiles` > 0): every pair
 // has `tiles` units, each for a tile (for more, if the pair has more tiles than that).
-// rows up to 64 take page_attn_few, more page_attn_many.
+// rows of 16 and 32 take page_attn_few, more page_attn_many.
 struct PagePlan {
   int32_t rows, units, step, tiles;
   int32_t item_keys;        // what an item's start and end cost, in keys

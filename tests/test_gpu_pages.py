@@ -191,6 +191,8 @@ SHAPES = [
     ([3, 0, 17, 5, 40], [3, 12, 700, 2, 41]),              # none, all of it, more than the length
     ([130, 1], [130, 333]),
     ([300], [1111]),
+    ([9, 4], [999, 70]),
+    ([18, 1, 16], [2100, 129, 16]),
 ]
 
 
