@@ -6,8 +6,8 @@
 // page_read    gives stored rows back as bf16.
 //
 // All three move each row once and are bound by HBM where there are many rows, by
-// latency where there are few.  A wave takes one row: its 64 lanes hold 64
-// pieces of eight channels (16 bytes), that is 512 / d heads at a time.
+// latency where there are few.  The 64 lanes of a wave hold 64 pieces of eight
+// channels (16 bytes) of a row, that is 512 / d heads at a time.
 //
 // Rotation: x'_j = x_j cos a_j - x_{j + d/2} sin a_j, x'_{j + d/2} = x_{j + d/2}
 // cos a_j + x_j sin a_j, a_j = p theta^(-2j/d), all in fp64 (positions of a long
@@ -152,73 +152,179 @@ __device__ __forceinline__ uint4 load_v(const uint8_t *block, int rows, int r, i
   }
 }
 
-// The sequence of stacked row `row` (-1: none), found by the whole wave: the last
-// b with row_start[b] <= row, if the row lies before its end.  Each round the
-// lanes probe 64 evenly spaced starts.
-__device__ __forceinline__ int seq_of_row(const PageSeqs &s, int row) {
-  if (s.row_start == nullptr) return row;
-  const int lane = threadIdx.x & 63;
-  int lo = 0, hi = s.n_seqs + 1;            // the first start beyond the row lies in [lo, hi]
-  while (lo < hi) {
-    const int step = (hi - lo + 63) / 64;
-    const int p = lo + (lane + 1) * step - 1;
-    const unsigned long long m = __ballot(p >= hi || s.row_start[p] > row);
-    if (m == 0ull) {
-      lo = hi;
-    } else {
-      const int k = __builtin_ctzll(m);
-      const int pk = lo + (k + 1) * step - 1;
-      lo += k * step;
-      hi = min(hi, pk);
+// Stores rows r .. r + 3 (r a multiple of 4) in FP4, eight channels a lane, with four
+// stores: the four rows' codes of V are neighbours, and so are four lanes' codes of a row
+// of K, which the lanes of a block exchange (lane y of the four gets row r + y).
+template <int D>
+__device__ __forceinline__ void store_four(uint8_t *block, int rows, int r, int piece, const uint4 *x, const uint4 *y,
+                                           bool on) {
+  using B = PageBlock<D, true>;
+  uint32_t kc[4], vc[4], ks[4], vs = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    ks[u] = fp4_scale(x[u]);
+    kc[u] = fp4_codes(x[u], ks[u]);
+    const uint32_t s = fp4_scale(y[u]);
+    vc[u] = fp4_codes(y[u], s);
+    vs |= s << (8 * u);
+  }
+  // a transpose of 4 x 4 over the rows (registers) and the block's lanes
+  const int q = piece & 3;
+#pragma unroll
+  for (int b = 1; b <= 2; b *= 2) {
+    const bool high = (q & b) != 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (u & b) continue;
+      const uint32_t give = high ? kc[u] : kc[u | b];
+      const uint32_t got = (uint32_t)__shfl_xor((int)give, b);
+      if (high) kc[u] = got; else kc[u | b] = got;
     }
   }
-  return lo > s.n_seqs ? -1 : lo - 1;
-}
-
-// Where stacked row `row` is stored: its sequence's page and its row there.
-// page < 0: nowhere.  Wave-uniform.
-struct Place {
-  int page, r;
-  bool mine;                // the row belongs to a sequence
-};
-__device__ __forceinline__ Place place_of(const PagePool &p, const PageSeqs &s, int row) {
-  Place x = {-1, 0, false};
-  const int b = __builtin_amdgcn_readfirstlane(seq_of_row(s, row));
-  if (b < 0) return x;
-  const PageSeq q = page_seq(p, s, b);
-  if (row < q.r0 || row >= q.r0 + q.n) return x;    // (starts that fall)
-  x.mine = true;
-  const int t = q.len - q.n + (row - q.r0);
-  if (t < 0) return x;
-  const int id = s.tables[(int64_t)b * s.max_pages + (t >> p.log_rows)];
-  if (id < 0 || id >= p.n_pages) {
-    page_note(p, HERMES_PAGE_BAD_ID);
-    return x;
+  const uint32_t scale = q == 0 ? ks[0] : q == 1 ? ks[1] : q == 2 ? ks[2] : ks[3];
+  if (!on) return;
+  *reinterpret_cast<uint4 *>(block + B::k(r + q) + 16 * (piece / 4)) = uint4{kc[0], kc[1], kc[2], kc[3]};
+  block[B::ks(rows, r + q) + piece / 4] = (uint8_t)scale;
+  if constexpr (D == 128) {
+    *reinterpret_cast<uint4 *>(block + B::v(rows, r / 4) + 16 * piece) = uint4{vc[0], vc[1], vc[2], vc[3]};
+  } else {                                  // (two pieces of four channels)
+    *reinterpret_cast<uint4 *>(block + B::v(rows, r / 4) + 16 * piece) =
+        uint4{(vc[0] & 0xFFFFu) | vc[1] << 16, (vc[2] & 0xFFFFu) | vc[3] << 16, vc[0] >> 16 | (vc[1] & 0xFFFF0000u),
+              vc[2] >> 16 | (vc[3] & 0xFFFF0000u)};
   }
-  x.page = __builtin_amdgcn_readfirstlane(id);
-  x.r = __builtin_amdgcn_readfirstlane(t & ((1 << p.log_rows) - 1));
-  return x;
+  if (q == 0) *reinterpret_cast<uint32_t *>(block + B::vs(rows, r / 4) + piece / 4 * 4) = vs;
 }
 
+// Finds where stacked rows are stored; every call is the whole wave's, and its results
+// are the same in every lane.
+struct Finder {
+  const PagePool &pool;
+  const PageSeqs &seqs;
+  int start, len;           // with up to 63 sequences: lane b has row_start[b] and kv_len[b]
+  int b;                    // else: the last row's sequence
+  PageSeq seq;
+
+  __device__ __forceinline__ Finder(const PagePool &p, const PageSeqs &s) : pool(p), seqs(s), start(0), len(0), b(-1) {
+    seq = PageSeq{0, 0, 0};
+    if (lanes()) {
+      const int lane = threadIdx.x & 63;
+      if (s.row_start != nullptr && lane <= s.n_seqs) start = s.row_start[lane];
+      if (lane < s.n_seqs) len = s.kv_len[lane];
+    }
+  }
+  __device__ __forceinline__ bool lanes() const { return seqs.n_seqs < 64; }
+
+  // The sequence of row `row` (-1: none): the last b with row_start[b] <= row.  Each round
+  // of the search the lanes probe 64 evenly spaced starts.
+  __device__ __forceinline__ int seq_of(int row) const {
+    if (seqs.row_start == nullptr) return row;
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = seqs.n_seqs + 1;       // the first start beyond the row lies in [lo, hi]
+    if (lanes()) {
+      const unsigned long long m = __ballot(lane >= hi || start > row);
+      lo = m == 0ull ? hi : min((int)__builtin_ctzll(m), hi);
+    } else {
+      while (lo < hi) {
+        const int step = (hi - lo + 63) / 64;
+        const int p = lo + (lane + 1) * step - 1;
+        const unsigned long long m = __ballot(p >= hi || seqs.row_start[p] > row);
+        if (m == 0ull) {
+          lo = hi;
+        } else {
+          const int k = __builtin_ctzll(m);
+          const int pk = lo + (k + 1) * step - 1;
+          lo += k * step;
+          hi = min(hi, pk);
+        }
+      }
+    }
+    return lo > seqs.n_seqs ? -1 : __builtin_amdgcn_readfirstlane(lo - 1);
+  }
+
+  // A row's sequence b, and its token t there (t < 0: not stored); false: in none.
+  __device__ __forceinline__ bool token_of(int row, int *t) {
+    if (b < 0 || seqs.row_start == nullptr || lanes() || row < seq.r0 || row >= seq.r0 + seq.n) {
+      b = seq_of(row);
+      if (b < 0) return false;
+      if (lanes()) {
+        // (as page_seq, from the lanes)
+        int a0 = b, a1 = b + 1;
+        if (seqs.row_start != nullptr) {
+          a0 = __builtin_amdgcn_readlane(start, b);
+          a1 = __builtin_amdgcn_readlane(start, b + 1);
+        }
+        seq = page_seq_of(pool, seqs, a0, a1, __builtin_amdgcn_readlane(len, b));
+      } else {
+        const PageSeq x = page_seq(pool, seqs, b);
+        seq = PageSeq{__builtin_amdgcn_readfirstlane(x.r0), __builtin_amdgcn_readfirstlane(x.n),
+                      __builtin_amdgcn_readfirstlane(x.len)};
+      }
+    }
+    if (row < seq.r0 || row >= seq.r0 + seq.n) return false;   // (starts that fall)
+    *t = seq.len - seq.n + (row - seq.r0);
+    return true;
+  }
+
+  // The page of token t of sequence b: its id as the table has it (t < 0: -1).
+  __device__ __forceinline__ int id_of(int t) const {
+    return t < 0 ? -1 : seqs.tables[(int64_t)b * seqs.max_pages + (t >> pool.log_rows)];
+  }
+  // and checked (-1: none)
+  __device__ __forceinline__ int checked(int t, int id) const {
+    if (t < 0) return -1;
+    if (id < 0 || id >= pool.n_pages) {
+      page_note(pool, HERMES_PAGE_BAD_ID);
+      return -1;
+    }
+    return __builtin_amdgcn_readfirstlane(id);
+  }
+};
+
+// A row's passes (512 / d heads of q each, then of k and v) are shared by a.share waves: one
+// where the rows fill the device, four where they do not and a row's latency counts
+// (16 rows of 28 + 4 heads of 128: 7.5 us with one wave a row).
+constexpr int kAhead = 4;           // passes of q whose loads are on their way at once
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
   constexpr int HD = D / 2, CH = D / 8, HP = 64 / CH;    // pieces of a head, heads of a pass
   __shared__ double2 trig[NT / 64][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int row = blockIdx.x * (NT / 64) + wave;
+  const int share = a.share, nth = wave % share;
+  const int row = blockIdx.x * (NT / 64 / share) + wave / share;
   if (row >= a.seqs.n_rows) return;
-  const Place at = place_of(a.pool, a.seqs, row);
-  if (!at.mine) return;
-  const int Hq = a.pool.Hq, Hkv = a.pool.Hkv;
+  const int Hq = a.q != nullptr ? a.pool.Hq : 0, Hkv = a.pool.Hkv;
+  const int q_passes = (Hq + HP - 1) / HP;
   const int piece = lane % CH, hl = lane / CH;
   const bool turn = a.rope != nullptr, second = piece >= CH / 2;
   const int f0 = 8 * (piece % (CH / 2));
+  const uint16_t *q = a.q + (int64_t)row * a.q_stride;
+  const uint16_t *k = a.k + (int64_t)row * a.k_stride, *v = a.v + (int64_t)row * a.v_stride;
+
+  int pos = 0;
+  double freq = 0.0;
   if (turn) {
     const int f = lane % HD;
     const int axis = a.axes != 3 ? 0 : f < a.section[0] ? 0 : f < a.section[0] + a.section[1] ? 1 : 2;
-    const int p = a.rope[(int64_t)axis * a.seqs.n_rows + row];
+    pos = a.rope[(int64_t)axis * a.seqs.n_rows + row];
+    freq = a.inv_freq[f];
+  }
+  Finder find(a.pool, a.seqs);
+  // the wave's first passes of q are asked for before the row's place is known
+  auto load_q = [&](uint4 *x, int pass0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = (pass0 + u * share) * HP + hl;
+      if (h < Hq) x[u] = *reinterpret_cast<const uint4 *>(q + h * D + 8 * piece);
+    }
+  };
+  uint4 x[kAhead];
+  load_q(x, nth);
+  int t = -1;
+  if (!find.token_of(row, &t)) return;
+  const int id = find.id_of(t);
+  if (turn) {
     double sn, cs;
-    sincos((double)p * a.inv_freq[f], &sn, &cs);
+    sincos((double)pos * freq, &sn, &cs);
     trig[wave][lane] = double2{cs, sn};
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
   }
@@ -231,97 +337,130 @@ __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
       w[i] = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const double2 t = trig[wave][f0 + 2 * i + h];
+        const double2 c = trig[wave][f0 + 2 * i + h];
         const double xd = bf16_to_f64((uint16_t)(xw[i] >> (16 * h))), yd = bf16_to_f64((uint16_t)(yw[i] >> (16 * h)));
-        const double xc = __dmul_rn(xd, t.x), ys = __dmul_rn(yd, t.y);
+        const double xc = __dmul_rn(xd, c.x), ys = __dmul_rn(yd, c.y);
         w[i] |= f64_to_bf16(second ? __dadd_rn(xc, ys) : __dsub_rn(xc, ys)) << (16 * h);
       }
     }
     return uint4{w[0], w[1], w[2], w[3]};
   };
-  if (a.q != nullptr) {
-    const uint16_t *q = a.q + (int64_t)row * a.q_stride;
-    uint16_t *o = a.q_out + (int64_t)row * Hq * D;
-    for (int h0 = 0; h0 < Hq; h0 += HP) {
-      const int e = (h0 + hl) * D + 8 * piece;
-      const bool on = h0 + hl < Hq;
-      uint4 x = {0u, 0u, 0u, 0u};
-      if (on) x = *reinterpret_cast<const uint4 *>(q + e);
-      x = rotated(x);
-      if (on) *reinterpret_cast<uint4 *>(o + e) = x;
+  const int page_id = find.checked(t, id);
+  const int rows = 1 << a.pool.log_rows, r = t & (rows - 1);
+  uint8_t *page = a.pool.pages + (int64_t)max(page_id, 0) * a.pool.page_bytes;
+  uint16_t *o = a.q_out + (int64_t)row * Hq * D;
+  for (int pass0 = nth; pass0 < q_passes; pass0 += kAhead * share) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = (pass0 + u * share) * HP + hl;
+      if (pass0 + u * share >= q_passes) break;
+      const uint4 z = rotated(x[u]);
+      if (h < Hq) *reinterpret_cast<uint4 *>(o + h * D + 8 * piece) = z;
     }
+    load_q(x, pass0 + kAhead * share);
   }
-  if (at.page < 0) return;
-  const int rows = 1 << a.pool.log_rows;
-  uint8_t *page = a.pool.pages + (int64_t)at.page * a.pool.page_bytes;
-  const uint16_t *k = a.k + (int64_t)row * a.k_stride, *v = a.v + (int64_t)row * a.v_stride;
-  for (int h0 = 0; h0 < Hkv; h0 += HP) {
-    const int h = h0 + hl, e = h * D + 8 * piece;
-    const bool on = h < Hkv;
-    uint4 x = {0u, 0u, 0u, 0u}, y = {0u, 0u, 0u, 0u};
-    if (on) {
-      x = *reinterpret_cast<const uint4 *>(k + e);
-      y = *reinterpret_cast<const uint4 *>(v + e);
+  // (the passes of k and v go on where those of q ended, so that the waves have equal shares)
+  const int first = (nth + share - q_passes % share) % share;
+  for (int pass = first; pass * HP < Hkv; pass += share) {
+    const int h = pass * HP + hl, e = h * D + 8 * piece;
+    uint4 kx = {0u, 0u, 0u, 0u}, vx = {0u, 0u, 0u, 0u};
+    if (h < Hkv) {
+      kx = *reinterpret_cast<const uint4 *>(k + e);
+      vx = *reinterpret_cast<const uint4 *>(v + e);
     }
-    if (turn) x = rotated(x);
+    if (turn) kx = rotated(kx);
+    const bool on = h < Hkv && page_id >= 0;
     uint8_t *block = page + (int64_t)h * a.pool.block_bytes;
-    store_k<D, FP4>(block, rows, at.r, piece, x, on);
-    store_v<D, FP4>(block, rows, at.r, piece, y, on);
+    store_k<D, FP4>(block, rows, r, piece, kx, on);
+    store_v<D, FP4>(block, rows, r, piece, vx, on);
   }
 }
 
+// A wave reads four rows, so that the loads of all are on their way at once: the chain of
+// starts, table and page took 77 us for 28 layers' 114688 rows with a row a wave.
+constexpr int RR = 4;
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_read(PageReadArgs a) {
   constexpr int CH = D / 8, HP = 64 / CH;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int row = blockIdx.x * (NT / 64) + wave;
-  if (row >= a.seqs.n_rows) return;
-  const Place at = place_of(a.pool, a.seqs, row);
-  if (!at.mine) return;
+  const int row0 = (blockIdx.x * (NT / 64) + wave) * RR;
+  if (row0 >= a.seqs.n_rows) return;
   const int Hkv = a.pool.Hkv, piece = lane % CH, hl = lane / CH;
   const int rows = 1 << a.pool.log_rows;
-  const uint8_t *page = a.pool.pages + (int64_t)max(at.page, 0) * a.pool.page_bytes;
+  Finder find(a.pool, a.seqs);
+  bool mine[RR];
+  int t[RR], id[RR];
+#pragma unroll
+  for (int u = 0; u < RR; ++u) {
+    t[u] = -1;
+    mine[u] = row0 + u < a.seqs.n_rows && find.token_of(row0 + u, &t[u]);
+    id[u] = mine[u] ? find.id_of(t[u]) : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < RR; ++u) id[u] = mine[u] ? find.checked(t[u], id[u]) : -1;
   for (int h = hl; h < Hkv; h += HP) {
-    const int64_t e = ((int64_t)row * Hkv + h) * D + 8 * piece;
-    const uint8_t *block = page + (int64_t)h * a.pool.block_bytes;
-    uint4 x = {0u, 0u, 0u, 0u}, y = {0u, 0u, 0u, 0u};
-    if (at.page >= 0) {
-      x = load_k<D, FP4>(block, rows, at.r, piece);
-      y = load_v<D, FP4>(block, rows, at.r, piece);
+    uint4 x[RR], y[RR];
+#pragma unroll
+    for (int u = 0; u < RR; ++u) {
+      x[u] = y[u] = uint4{0u, 0u, 0u, 0u};
+      if (id[u] >= 0) {
+        const uint8_t *block = a.pool.pages + (int64_t)id[u] * a.pool.page_bytes + (int64_t)h * a.pool.block_bytes;
+        x[u] = load_k<D, FP4>(block, rows, t[u] & (rows - 1), piece);
+        y[u] = load_v<D, FP4>(block, rows, t[u] & (rows - 1), piece);
+      }
     }
-    if (a.k != nullptr) *reinterpret_cast<uint4 *>(a.k + e) = x;
-    if (a.v != nullptr) *reinterpret_cast<uint4 *>(a.v + e) = y;
+#pragma unroll
+    for (int u = 0; u < RR; ++u) {
+      if (!mine[u]) continue;
+      const int64_t e = ((int64_t)(row0 + u) * Hkv + h) * D + 8 * piece;
+      if (a.k != nullptr) *reinterpret_cast<uint4 *>(a.k + e) = x[u];
+      if (a.v != nullptr) *reinterpret_cast<uint4 *>(a.v + e) = y[u];
+    }
   }
 }
 
+// A wave packs four rows, which lie in one page and are one group of V's layout.
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_pack(PagePackArgs a) {
   constexpr int CH = D / 8, HP = 64 / CH;
   const int j = blockIdx.y, len = a.len[j];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.kv_len[j] = len;
-  const int row = blockIdx.x * (NT / 64) + wave;
-  if (row >= len) return;
-  const int id = a.tables[(int64_t)j * a.max_pages + (row >> a.pool.log_rows)];
-  if (id < 0 || id >= a.pool.n_pages) {
-    page_note(a.pool, HERMES_PAGE_BAD_ID);
-    return;
-  }
+  const int row0 = (blockIdx.x * (NT / 64) + wave) * 4;
+  if (row0 >= len) return;
+  int id = a.tables[(int64_t)j * a.max_pages + (row0 >> a.pool.log_rows)];
   const int Hkv = a.pool.Hkv, piece = lane % CH, hl = lane / CH;
-  const int rows = 1 << a.pool.log_rows, r = row & (rows - 1);
-  uint8_t *page = a.pool.pages + (int64_t)__builtin_amdgcn_readfirstlane(id) * a.pool.page_bytes;
-  const uint16_t *k = a.k[j] + (int64_t)row * Hkv * D, *v = a.v[j] + (int64_t)row * Hkv * D;
+  const int rows = 1 << a.pool.log_rows, r = row0 & (rows - 1);
+  const uint16_t *k = a.k[j] + (int64_t)row0 * Hkv * D, *v = a.v[j] + (int64_t)row0 * Hkv * D;
   for (int h0 = 0; h0 < Hkv; h0 += HP) {
     const int h = h0 + hl, e = h * D + 8 * piece;
-    const bool on = h < Hkv;
-    uint4 x = {0u, 0u, 0u, 0u}, y = {0u, 0u, 0u, 0u};
-    if (on) {
-      x = *reinterpret_cast<const uint4 *>(k + e);
-      y = *reinterpret_cast<const uint4 *>(v + e);
+    uint4 x[4], y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      x[u] = y[u] = uint4{0u, 0u, 0u, 0u};
+      if (h < Hkv && row0 + u < len) {
+        x[u] = *reinterpret_cast<const uint4 *>(k + (int64_t)u * Hkv * D + e);
+        y[u] = *reinterpret_cast<const uint4 *>(v + (int64_t)u * Hkv * D + e);
+      }
     }
-    uint8_t *block = page + (int64_t)h * a.pool.block_bytes;
-    store_k<D, FP4>(block, rows, r, piece, x, on);
-    store_v<D, FP4>(block, rows, r, piece, y, on);
+    if (h0 == 0) {
+      id = __builtin_amdgcn_readfirstlane(id);
+      if (id < 0 || id >= a.pool.n_pages) {
+        page_note(a.pool, HERMES_PAGE_BAD_ID);
+        return;
+      }
+    }
+    uint8_t *block = a.pool.pages + (int64_t)id * a.pool.page_bytes + (int64_t)h * a.pool.block_bytes;
+    if (FP4 && row0 + 4 <= len) {
+      store_four<D>(block, rows, r, piece, x, y, h < Hkv);
+      continue;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool on = h < Hkv && row0 + u < len;
+      store_k<D, FP4>(block, rows, r + u, piece, x[u], on);
+      store_v<D, FP4>(block, rows, r + u, piece, y[u], on);
+    }
   }
 }
 
@@ -340,14 +479,16 @@ hipError_t with_kind(int head_dim, int format, F &&fn) {
 }  // namespace
 
 hipError_t launch_page_append(const PageAppendArgs &a, int head_dim, int format, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)a.seqs.n_rows + NT / 64 - 1) / (NT / 64)));
+  const int per = NT / 64 / a.share;
+  const dim3 grid((unsigned)((a.seqs.n_rows + per - 1) / per));
   return with_kind(head_dim, format, [&](auto d, auto f) {
     hipLaunchKernelGGL((page_append<decltype(d)::value, decltype(f)::value>), grid, dim3(NT), 0, s, a);
   });
 }
 
 hipError_t launch_page_read(const PageReadArgs &a, int head_dim, int format, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)a.seqs.n_rows + NT / 64 - 1) / (NT / 64)));
+  constexpr int per = NT / 64 * RR;
+  const dim3 grid((unsigned)((a.seqs.n_rows + per - 1) / per));
   return with_kind(head_dim, format, [&](auto d, auto f) {
     hipLaunchKernelGGL((page_read<decltype(d)::value, decltype(f)::value>), grid, dim3(NT), 0, s, a);
   });
@@ -356,7 +497,8 @@ hipError_t launch_page_read(const PageReadArgs &a, int head_dim, int format, hip
 hipError_t launch_page_pack(const PagePackArgs &a, int head_dim, int format, hipStream_t s) {
   int most = 1;                                        // (an empty layer's length is written too)
   for (int j = 0; j < a.n_list; ++j) most = max(most, a.len[j]);
-  const dim3 grid((unsigned)(((int64_t)most + NT / 64 - 1) / (NT / 64)), a.n_list);
+  constexpr int per = NT / 64 * 4;
+  const dim3 grid((unsigned)(((int64_t)most + per - 1) / per), a.n_list);
   return with_kind(head_dim, format, [&](auto d, auto f) {
     hipLaunchKernelGGL((page_pack<decltype(d)::value, decltype(f)::value>), grid, dim3(NT), 0, s, a);
   });

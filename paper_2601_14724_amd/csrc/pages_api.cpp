@@ -186,6 +186,7 @@ int hermes_page_append(const hermes_page_pool *pool, const hermes_page_batch *ba
   a.k_stride = k_stride;
   a.v_stride = v_stride;
   a.rope = rope;
+  a.share = batch->n_rows < 4 * kStreamSlots ? 4 : 1;   // (a row a wave fills the CUs from there on)
   if (rope != nullptr) fill_rope(pool, &a);
   return launch_page_append(a, pool->head_dim, pool->format, static_cast<hipStream_t>(stream)) == hipSuccess
              ? HERMES_OK : HERMES_EHIP;

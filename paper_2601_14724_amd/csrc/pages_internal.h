@@ -32,6 +32,7 @@ struct PageAppendArgs {
   const int32_t *rope;      // [axes][n_rows], or null: k as it is
   int32_t axes;
   int32_t section[3];       // axes 3: frequency pairs of the t, h, w sections
+  int32_t share;            // waves that share a row: 1 or 4
   double inv_freq[kMaxHalfDim];
 };
 
@@ -110,24 +111,22 @@ struct PageSeq {
 __device__ __forceinline__ void page_note(const PagePool &p, int bit) {
   if (p.status != nullptr) atomicOr(p.status, bit);
 }
-__device__ __forceinline__ PageSeq page_seq(const PagePool &p, const PageSeqs &s, int b) {
+__device__ __forceinline__ PageSeq page_seq_of(const PagePool &p, const PageSeqs &s, int a0, int a1, int len) {
   PageSeq x;
-  if (s.row_start != nullptr) {
-    const int a0 = s.row_start[b], a1 = s.row_start[b + 1];
-    x.r0 = min(max(a0, 0), s.n_rows);
-    const int r1 = min(max(a1, x.r0), s.n_rows);
-    x.n = r1 - x.r0;
-    if (x.r0 != a0 || r1 != a1) page_note(p, HERMES_PAGE_BAD_ROWS);
-  } else {
-    x.r0 = b;
-    x.n = 1;
-  }
-  x.len = s.kv_len[b];
-  if (x.len < 0 || x.len > (int64_t)s.max_pages << p.log_rows) {
+  x.r0 = min(max(a0, 0), s.n_rows);
+  const int r1 = min(max(a1, x.r0), s.n_rows);
+  x.n = r1 - x.r0;
+  if (x.r0 != a0 || r1 != a1) page_note(p, HERMES_PAGE_BAD_ROWS);
+  x.len = len;
+  if (len < 0 || len > (int64_t)s.max_pages << p.log_rows) {
     x.len = 0;
     page_note(p, HERMES_PAGE_BAD_LENGTH);
   }
   return x;
+}
+__device__ __forceinline__ PageSeq page_seq(const PagePool &p, const PageSeqs &s, int b) {
+  const bool starts = s.row_start != nullptr;
+  return page_seq_of(p, s, starts ? s.row_start[b] : b, starts ? s.row_start[b + 1] : b + 1, s.kv_len[b]);
 }
 // Byte offsets inside a KV head's block (see hermes.h): K row r, V rows 4 r4 ..
 // 4 r4 + 3, and their scales.

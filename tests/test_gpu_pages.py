@@ -110,6 +110,8 @@ APPENDS = [
     ((3, 3, 64), "fp4", 128, [10, 2], [130, 2], 3),
     ((12, 6, 128), "fp4", 32, [9], [33], 3),
     ((2, 1, 128), "bf16", 16, [4, 6], [2, 5], 3),        # more rows than the length: the first are not stored
+    ((4, 2, 64), "fp4", 16, [1 + 5 * (b % 3) for b in range(130)], [12 + b for b in range(130)], 1),
+    ((9, 9, 128), "bf16", 32, [0, 700, 0, 420, 3], [0, 900, 5, 420, 64], 1),
 ]
 
 
@@ -222,6 +224,15 @@ def test_attend_does_not_depend_on_the_hints(max_rows, max_len, d):
 def test_attend_sharp_scores(fmt):
     """Scores of some hundreds: the running maximum moves, and most of P underflows."""
     s = Setup((8, 2, 128), fmt, 64, [1, 50], [3000, 1500], seed=9, scale=6.0)
+    lse = torch.empty((s.n, s.hq), device=DEV)
+    s.check_attend(s.pool.attend(s.batch, dev(s.q), lse=lse), lse)
+
+
+@pytest.mark.parametrize("max_rows", [1, 3, 40])
+def test_attend_many_sequences(max_rows):
+    """More sequences than lanes, some without rows, some without tokens."""
+    rows, lens = [b * 7 % 4 for b in range(150)], [b * 37 % 400 for b in range(150)]
+    s = Setup((8, 2, 64), "fp4", 16, rows, lens, seed=10).hints(max_rows, 5000)
     lse = torch.empty((s.n, s.hq), device=DEV)
     s.check_attend(s.pool.attend(s.batch, dev(s.q), lse=lse), lse)
 
