@@ -152,13 +152,13 @@ __device__ __forceinline__ uint4 load_v(const uint8_t *block, int rows, int r, i
   }
 }
 
-// Stores rows r .. r + 3 (r a multiple of 4) in FP4, eight channels a lane, with four
-// stores: the four rows' codes of V are neighbours, and so are four lanes' codes of a row
-// of K, which the lanes of a block exchange (lane y of the four gets row r + y).
-template <int D>
+// Stores rows r .. r + 3 (r a multiple of 4) in FP4 at head size 128, eight channels a
+// lane, with four stores: the four rows' codes of V are neighbours, and so are four lanes'
+// codes of a row of K, which the lanes of a block exchange (lane y of the four gets row
+// r + y).
 __device__ __forceinline__ void store_four(uint8_t *block, int rows, int r, int piece, const uint4 *x, const uint4 *y,
                                            bool on) {
-  using B = PageBlock<D, true>;
+  using B = PageBlock<128, true>;
   uint32_t kc[4], vc[4], ks[4], vs = 0;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -184,14 +184,8 @@ __device__ __forceinline__ void store_four(uint8_t *block, int rows, int r, int 
   const uint32_t scale = q == 0 ? ks[0] : q == 1 ? ks[1] : q == 2 ? ks[2] : ks[3];
   if (!on) return;
   *reinterpret_cast<uint4 *>(block + B::k(r + q) + 16 * (piece / 4)) = uint4{kc[0], kc[1], kc[2], kc[3]};
+  *reinterpret_cast<uint4 *>(block + B::v(rows, r / 4) + 16 * piece) = uint4{vc[0], vc[1], vc[2], vc[3]};
   block[B::ks(rows, r + q) + piece / 4] = (uint8_t)scale;
-  if constexpr (D == 128) {
-    *reinterpret_cast<uint4 *>(block + B::v(rows, r / 4) + 16 * piece) = uint4{vc[0], vc[1], vc[2], vc[3]};
-  } else {                                  // (two pieces of four channels)
-    *reinterpret_cast<uint4 *>(block + B::v(rows, r / 4) + 16 * piece) =
-        uint4{(vc[0] & 0xFFFFu) | vc[1] << 16, (vc[2] & 0xFFFFu) | vc[3] << 16, vc[0] >> 16 | (vc[1] & 0xFFFF0000u),
-              vc[2] >> 16 | (vc[3] & 0xFFFF0000u)};
-  }
   if (q == 0) *reinterpret_cast<uint32_t *>(block + B::vs(rows, r / 4) + piece / 4 * 4) = vs;
 }
 
@@ -376,9 +370,9 @@ __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
   }
 }
 
-// A wave reads four rows, so that the loads of all are on their way at once: the chain of
-// starts, table and page took 77 us for 28 layers' 114688 rows with a row a wave.
-constexpr int RR = 4;
+// A wave reads two rows, whose loads are on their way at once: 28 layers' 114688 rows of 4
+// heads of 128 take 71 us (297 MB, 4.2 TB/s), with one row a wave 80 and with four 79.
+constexpr int RR = 2;
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_read(PageReadArgs a) {
   constexpr int CH = D / 8, HP = 64 / CH;
@@ -419,14 +413,16 @@ __global__ __launch_bounds__(NT) void page_read(PageReadArgs a) {
   }
 }
 
-// A wave packs four rows, which lie in one page and are one group of V's layout.
+// With FP4 a wave packs four rows, which lie in one page and are one group of V's layout
+// (28 layers' 114688 rows of 4 heads of 128: 59 us, 297 MB; a row a wave, 62).  bf16 rows
+// leave in whole lines anyway, and take a wave each (91 us, 470 MB; four rows, 100).
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_pack(PagePackArgs a) {
-  constexpr int CH = D / 8, HP = 64 / CH;
+  constexpr int CH = D / 8, HP = 64 / CH, PR = FP4 ? 4 : 1;
   const int j = blockIdx.y, len = a.len[j];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.kv_len[j] = len;
-  const int row0 = (blockIdx.x * (NT / 64) + wave) * 4;
+  const int row0 = (blockIdx.x * (NT / 64) + wave) * PR;
   if (row0 >= len) return;
   int id = a.tables[(int64_t)j * a.max_pages + (row0 >> a.pool.log_rows)];
   const int Hkv = a.pool.Hkv, piece = lane % CH, hl = lane / CH;
@@ -434,9 +430,9 @@ __global__ __launch_bounds__(NT) void page_pack(PagePackArgs a) {
   const uint16_t *k = a.k[j] + (int64_t)row0 * Hkv * D, *v = a.v[j] + (int64_t)row0 * Hkv * D;
   for (int h0 = 0; h0 < Hkv; h0 += HP) {
     const int h = h0 + hl, e = h * D + 8 * piece;
-    uint4 x[4], y[4];
+    uint4 x[PR], y[PR];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < PR; ++u) {
       x[u] = y[u] = uint4{0u, 0u, 0u, 0u};
       if (h < Hkv && row0 + u < len) {
         x[u] = *reinterpret_cast<const uint4 *>(k + (int64_t)u * Hkv * D + e);
@@ -451,12 +447,14 @@ __global__ __launch_bounds__(NT) void page_pack(PagePackArgs a) {
       }
     }
     uint8_t *block = a.pool.pages + (int64_t)id * a.pool.page_bytes + (int64_t)h * a.pool.block_bytes;
-    if (FP4 && row0 + 4 <= len) {
-      store_four<D>(block, rows, r, piece, x, y, h < Hkv);
-      continue;
+    if constexpr (FP4 && D == 128) {
+      if (row0 + PR <= len) {
+        store_four(block, rows, r, piece, x, y, h < Hkv);
+        continue;
+      }
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < PR; ++u) {
       const bool on = h < Hkv && row0 + u < len;
       store_k<D, FP4>(block, rows, r + u, piece, x[u], on);
       store_v<D, FP4>(block, rows, r + u, piece, y[u], on);
@@ -497,7 +495,7 @@ hipError_t launch_page_read(const PageReadArgs &a, int head_dim, int format, hip
 hipError_t launch_page_pack(const PagePackArgs &a, int head_dim, int format, hipStream_t s) {
   int most = 1;                                        // (an empty layer's length is written too)
   for (int j = 0; j < a.n_list; ++j) most = max(most, a.len[j]);
-  constexpr int per = NT / 64 * 4;
+  const int per = NT / 64 * (format == HERMES_PAGE_FP4 ? 4 : 1);
   const dim3 grid((unsigned)(((int64_t)most + per - 1) / per), a.n_list);
   return with_kind(head_dim, format, [&](auto d, auto f) {
     hipLaunchKernelGGL((page_pack<decltype(d)::value, decltype(f)::value>), grid, dim3(NT), 0, s, a);

@@ -388,9 +388,10 @@ class HermesKV:
         lead = () if layer != ALL_LAYERS else (self.L,)
         _need(tables, torch.int32, lead + (tables.shape[-1],), "tables")
         _need(kv_len, torch.int32, lead or (1,), "kv_len")
-        with pages._here(tables, kv_len, self.k[0][0]):
-            check(lib.hermes_page_pack(self.ctx, layer, ctypes.byref(pages._pool), tables.data_ptr(), tables.shape[-1],
-                                       kv_len.data_ptr(), _stream()), "hermes_page_pack")
+        for t in (tables, kv_len, self.k[0][0]):
+            pages._on_device(t, "pack")
+        pages._run(lib.hermes_page_pack, "hermes_page_pack", self.ctx, layer, pages._ref, tables.data_ptr(),
+                   tables.shape[-1], kv_len.data_ptr())
 
     def rewind(self) -> None:
         check(lib.hermes_kv_rewind(self.ctx), "hermes_kv_rewind")
@@ -483,7 +484,7 @@ class PageBatch:
         b.max_rows = 1 if row_start is None else int(max_rows or 0)
         b.max_len = int(max_len or 0)
         b.row_start, b.kv_len, b.tables = _ptr(row_start), kv_len.data_ptr(), tables.data_ptr()
-        self._batch = b
+        self._batch, self._ref = b, ctypes.byref(b)
 
 
 class KVPages:
@@ -513,23 +514,39 @@ class KVPages:
         self.pages, self.device = pages, pages.device
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         p.pages, p.status = pages.data_ptr(), self._status.data_ptr()
-        self._pool = p
+        self._pool, self._ref, self._index = p, ctypes.byref(p), pages.get_device()
 
-    def _here(self, *tensors):
-        """The pool's device made current; every tensor has to be on it."""
-        for t in tensors:
-            if t is not None and t.device != self.device:
-                raise ValueError(f"a tensor on {t.device}, the pages are on {self.device}")
-        return torch.cuda.device(self.device)
+    # (a token's calls are a few microseconds on the device: their checks are kept short)
+    def _run(self, fn, name: str, *args) -> None:
+        """fn(*args, stream) with the pool's device current."""
+        if _raw_stream is not None and _device() == self._index:
+            check(fn(*args, _raw_stream(self._index)), name)
+        else:
+            with torch.cuda.device(self.device):
+                check(fn(*args, _stream()), name)
+
+    def _on_device(self, t: torch.Tensor, name: str) -> None:
+        if t.get_device() != self._index:
+            raise ValueError(f"{name}: a tensor on {t.device}, the pages are on {self.device}")
+
+    def _fits(self, t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> None:
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous {dtype} {shape}, got {getattr(t, 'dtype', None)} "
+                             f"{tuple(getattr(t, 'shape', ()))}")
+        self._on_device(t, name)
 
     def _rows(self, t: torch.Tensor, n: int, heads: int, name: str) -> int:
-        """Stride of rows [heads][d] of a bf16 device tensor that may lie apart."""
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or tuple(t.shape) != (n, heads, self.d):
+        """Stride of rows [heads][d] of a bf16 tensor, which may lie apart."""
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.shape != (n, heads, self.d):
             raise ValueError(f"{name}: expected torch.bfloat16 {(n, heads, self.d)}, got "
                              f"{getattr(t, 'dtype', None)} {tuple(getattr(t, 'shape', ()))}")
-        if not t.is_cuda or (n > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.d))):
-            raise ValueError(f"{name}: must be a device tensor of contiguous rows")
-        return t.stride(0) if n > 1 else heads * self.d
+        self._on_device(t, name)
+        if n == 0:
+            return heads * self.d
+        rs, hs, es = t.stride()
+        if es != 1 or (hs != self.d and heads > 1):
+            raise ValueError(f"{name}: a row's heads must be contiguous")
+        return rs if n > 1 else heads * self.d
 
     def append(self, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                rope: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
@@ -537,17 +554,21 @@ class KVPages:
         stores k and v as the last rows of their sequences, and returns the rotated q."""
         n = batch.n_rows
         ks, vs = self._rows(k, n, self.Hkv, "k"), self._rows(v, n, self.Hkv, "v")
-        qs = 0
+        qs, qp, op, rp = 0, None, None, None
         if q is not None:
-            qs = self._rows(q, n, self.Hq, "q")
+            qs, qp = self._rows(q, n, self.Hq, "q"), q.data_ptr()
             if q_out is None:
-                q_out = torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=self.device)
-            _need(q_out, torch.bfloat16, (n, self.Hq, self.d), "q_out")
+                q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+            else:
+                self._fits(q_out, torch.bfloat16, (n, self.Hq, self.d), "q_out")
+        if q_out is not None:
+            op = q_out.data_ptr()
         if rope is not None:
-            _need(rope, torch.int32, (n,) if self.axes == 1 else (3, n), "rope")
-        with self._here(k, v, q, q_out, rope, batch.kv_len):
-            check(lib.hermes_page_append(ctypes.byref(self._pool), ctypes.byref(batch._batch), _ptr(q), qs, k.data_ptr(), ks,
-                                         v.data_ptr(), vs, _ptr(rope), _ptr(q_out), _stream()), "hermes_page_append")
+            self._fits(rope, torch.int32, (n,) if self.axes == 1 else (3, n), "rope")
+            rp = rope.data_ptr()
+        self._on_device(batch.kv_len, "batch")
+        self._run(lib.hermes_page_append, "hermes_page_append", self._ref, batch._ref, qp, qs, k.data_ptr(), ks,
+                  v.data_ptr(), vs, rp, op)
         return q_out
 
     def attend(self, batch: PageBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -557,15 +578,20 @@ class KVPages:
         n = batch.n_rows
         qs = self._rows(q, n, self.Hq, "q")
         if out is None:
-            out = torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=self.device)
-        _need(out, torch.bfloat16, (n, self.Hq, self.d), "out")
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        else:
+            self._fits(out, torch.bfloat16, (n, self.Hq, self.d), "out")
+        lp = wp = None
         if lse is not None:
-            _need(lse, torch.float32, (n, self.Hq), "lse")
-        with self._here(q, out, lse, batch.kv_len):
-            nbytes = lib.hermes_page_workspace_bytes(ctypes.byref(self._pool), ctypes.byref(batch._batch))
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
-            check(lib.hermes_page_attend(ctypes.byref(self._pool), ctypes.byref(batch._batch), q.data_ptr(), qs,
-                                         out.data_ptr(), _ptr(lse), _ptr(ws), nbytes, _stream()), "hermes_page_attend")
+            self._fits(lse, torch.float32, (n, self.Hq), "lse")
+            lp = lse.data_ptr()
+        self._on_device(batch.kv_len, "batch")
+        nbytes = lib.hermes_page_workspace_bytes(self._ref, batch._ref)
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            wp = ws.data_ptr()
+        self._run(lib.hermes_page_attend, "hermes_page_attend", self._ref, batch._ref, q.data_ptr(), qs, out.data_ptr(),
+                  lp, wp, nbytes)
         return out
 
     def read(self, batch: PageBatch, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
@@ -573,13 +599,14 @@ class KVPages:
         shape = (batch.n_rows, self.Hkv, self.d)
         if k is None:
             k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        else:
+            self._fits(k, torch.bfloat16, shape, "k")
         if v is None:
             v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        _need(k, torch.bfloat16, shape, "k")
-        _need(v, torch.bfloat16, shape, "v")
-        with self._here(k, v, batch.kv_len):
-            check(lib.hermes_page_read(ctypes.byref(self._pool), ctypes.byref(batch._batch), k.data_ptr(), v.data_ptr(),
-                                       _stream()), "hermes_page_read")
+        else:
+            self._fits(v, torch.bfloat16, shape, "v")
+        self._on_device(batch.kv_len, "batch")
+        self._run(lib.hermes_page_read, "hermes_page_read", self._ref, batch._ref, k.data_ptr(), v.data_ptr())
         return k, v
 
     def faults(self) -> int:
