@@ -27,7 +27,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NT = 512, NW = NT / 64;
 constexpr int KS = 32;                  // keys of a wave's step (page_attn_few)
 constexpr float kLowest = -3.0e38f;     // running maximum before the first key (finite: -inf minus it stays -inf)
 constexpr float kLn2 = 0.69314718055994531f;
@@ -330,8 +329,8 @@ __device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *p) {
   }
 }
 
-template <int D, bool FP4, int RT>
-__global__ __launch_bounds__(NT, 1) void page_attn_few(PageAttnArgs a) {
+template <int D, bool FP4, int RT, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void page_attn_few(PageAttnArgs a) {
   using B = PageBlock<D, FP4>;
   constexpr int KK = D / 32;                // MFMAs of S for each group of keys
   constexpr int PC = D / 16;                // channels of a piece of V
@@ -578,7 +577,7 @@ __global__ __launch_bounds__(NT, 1) void page_attn_few(PageAttnArgs a) {
               float4{o[t][i][j], o[t][i + 1][j], o[t][i + 2][j], o[t][i + 3][j]};
       }
       __syncthreads();
-      constexpr int TPR = NT / 16, CPT = D / TPR;                    // threads of a row, channels of a thread
+      constexpr int TPR = 4 * NW, CPT = D / TPR;                    // threads of a row, channels of a thread
       const int row = threadIdx.x / TPR, ch = threadIdx.x % TPR * CPT;
       const int p = p0 + 16 * t + row;
       if (p >= P) continue;
@@ -1133,8 +1132,11 @@ template <int D, bool FP4>
 hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   const dim3 grid(a.plan.units);
   const int rows = a.plan.rows;
-  if (rows == 16) hipLaunchKernelGGL((page_attn_few<D, FP4, 1>), grid, dim3(NT), 0, s, a);
-  else if (rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2>), grid, dim3(NT), 0, s, a);
+  const bool four = a.plan.step == 128;
+  if (rows == 16 && four) hipLaunchKernelGGL((page_attn_few<D, FP4, 1, 4>), grid, dim3(256), 0, s, a);
+  else if (rows == 16) hipLaunchKernelGGL((page_attn_few<D, FP4, 1, 8>), grid, dim3(512), 0, s, a);
+  else if (rows == 32 && four) hipLaunchKernelGGL((page_attn_few<D, FP4, 2, 4>), grid, dim3(256), 0, s, a);
+  else if (rows == 32) hipLaunchKernelGGL((page_attn_few<D, FP4, 2, 8>), grid, dim3(512), 0, s, a);
   else if (rows == 64) hipLaunchKernelGGL((page_attn_many<D, FP4, 2>), grid, dim3(MT), 0, s, a);
   else if (rows == 128) hipLaunchKernelGGL((page_attn_many<D, FP4, 4>), grid, dim3(MT), 0, s, a);
   else hipLaunchKernelGGL((page_attn_many<D, FP4, 8>), grid, dim3(MT), 0, s, a);

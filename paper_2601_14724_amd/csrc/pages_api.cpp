@@ -52,6 +52,8 @@ PageSeqs seqs_of(const hermes_page_batch *b) {
 
 int64_t over(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
+constexpr int kWholeSteps = 16;   // steps of a round's longest items without cuts, at most
+
 // The cut of an attention call, from what the host knows of it.
 PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
@@ -62,18 +64,27 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   PagePlan x;
   x.rows = P <= 16 ? 16 : P <= 32 ? 32 : P <= 64 ? 64 : P <= 128 ? 128 : 256;
   x.item_keys = x.rows > 32 ? 320 : p->format == HERMES_PAGE_FP4 ? 1024 : 512;
-  x.step = x.rows <= 32 ? 256 : x.rows <= 128 ? 128 : 64;   // (a step of all a workgroup's key groups)
-  // A workgroup of eight waves fits a CU.  Without cuts a launch takes rounds of items,
-  // with cuts its steps are shared out, at the price of a second launch.
-  const int64_t slots = kStreamSlots;
-  const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles, steps = over(max_len, x.step);
-  const int64_t spare = over(items, slots) * steps - over(items * steps, slots);
-  if (spare <= (x.rows <= 32 ? 8 : 4) && items <= 1 << 24) {
+  // Without cuts a launch takes rounds of items; with cuts its steps are shared out, whatever
+  // the lengths, at the price of a second launch and of the parts (5 to 10 us).  So there
+  // are none where the longest items' rounds are short, in keys, and cuts would save
+  // little of them even if all were as long.  A workgroup of eight waves fits a CU; of the
+  // few-row kernel also two of four, which hide the start of one item behind another's
+  // keys where there are items enough (256 sequences of 1000 tokens, 4 KV heads: 38 us, 50
+  // with eight).  A step is 32 keys for each wave, or a tile for each key group.
+  const bool few = x.rows <= 32;
+  const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles;
+  const bool four = few && items >= 2 * kStreamSlots;
+  const int64_t slots = four ? 2 * kStreamSlots : kStreamSlots, step = few ? 256 : x.rows <= 128 ? 128 : 64;
+  const int64_t longest = over(items, slots) * max_len * (four ? 2 : 1), shared = over(items * max_len, kStreamSlots);
+  if (longest <= kWholeSteps * step && longest - shared <= (few ? 8 : 4) * step && items <= 1 << 24) {
+    x.step = (int32_t)(four ? step / 2 : step);
     x.tiles = (int32_t)tiles;
     x.units = (int32_t)items;
   } else {
+    const int64_t steps = items * over(max_len, step);
+    x.step = (int32_t)step;
     x.tiles = 0;
-    x.units = (int32_t)(items * steps < slots ? items * steps : slots);
+    x.units = (int32_t)(steps < kStreamSlots ? steps : kStreamSlots);
   }
   x.inv_units = 1.0 / x.units;
   x.inv_group = 1.0 / (double)G;
