@@ -461,7 +461,7 @@ enum {
  *  status       device int32 the HERMES_PAGE_BAD_* bits are ORed into, or NULL.
  *               Nothing is read or written out of bounds, with or without it.
  *  n_q_heads, n_kv_heads, head_dim, sm_scale, rope_theta, rope_axes,
- *  mrope_section   as in hermes_config.
+ *  mrope_section   as in hermes_config (sm_scale, where it is given, 1e-30 to 1e30).
  */
 typedef struct {
   int32_t n_q_heads;
@@ -543,7 +543,7 @@ size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_pa
  * Causal attention of every sequence's rows over its pages: row i of n sees the
  * tokens 0 .. kv_len - n + i (its own among them, so they are appended first).
  *  q            device bf16, rows of n_q_heads x head_dim, q_stride elements apart.
- *  out          device bf16 [n_rows][n_q_heads][head_dim].
+ *  out          device bf16 [n_rows][n_q_heads][head_dim], apart from q.
  *  lse          device fp32 [n_rows][n_q_heads] or NULL: ln sum exp of the scaled
  *               scores (joins the result with that over other keys).
  *  workspace    device memory of hermes_page_workspace_bytes, 16-byte aligned (may be

@@ -195,89 +195,99 @@ struct Items {
 };
 
 // A unit's walk over its items: body(item, lo, hi, whole, slot) for each, with the keys
-// [lo, hi) of it that are the unit's.  Between items the walk's own state waits in
-// LDS, a copy a wave, so that it takes no registers from the body.
+// [lo, hi) of it that are the unit's.  The first wave finds the items and leaves them in
+// LDS for all: so the waves take the same way through the barriers whatever the lengths'
+// memory holds, and the walk's state takes no registers from the body.  (body has a barrier
+// after which no wave reads the item again.)
 struct Walk {
   Item it;
-  int64_t lo, hi;
+  int64_t lo, hi, q;        // the unit's run, and the length of all units' runs
+  int more;                 // whether `it` is an item
 };
 template <int WAVES, typename F>
 __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&body) {
-  __shared__ Walk state[WAVES];
+  __shared__ Walk walk;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items items(a);
   const int tiles = a.plan.tiles;           // > 0: no cuts, `tiles` units for each pair
-  if (tiles > 0) {
+  if (wave == 0) {
     Walk w;
-    const int pair = unit / tiles;
-    w.it.b = pair / a.pool.Hkv;
-    w.it.kv = pair - w.it.b * a.pool.Hkv;
-    w.it.seq = page_seq(a.pool, a.seqs, w.it.b);
-    w.it.P = w.it.seq.n * items.G;
-    w.it.p0 = (unit - pair * tiles) * a.plan.rows;
-    w.it.start = w.lo = 0;
-    w.it.end = w.hi = 1;
-    if (w.it.p0 >= w.it.P) return;
-    state[wave] = w;
-  } else {
-    PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
-    const Items::Scan first = items.scan(0);
-    const int64_t N = items.total(first);
-    const int64_t q = max((int64_t)((double)N * a.plan.inv_units) + 1, (int64_t)a.plan.step * items.G);
-    const int64_t lo = unit * q, hi = min(lo + q, N);
-    if (lo < hi) {
-      const Item it = items.find(lo, first);
-      // (the wave with the fewest steps) this unit holds the item's first cut
-      if (wave == WAVES - 1 && it.start < lo && it.start >= lo - q)
-        cut = PageCut{unit - 1, (int)over64(it.end - 1, q), it.start == lo - q ? 0 : 1, it.kv, it.seq.r0, it.p0, it.P, 0};
-      state[wave] = Walk{it, lo, hi};
+    if (tiles > 0) {
+      const int pair = unit / tiles;
+      w.it.b = pair / a.pool.Hkv;
+      w.it.kv = pair - w.it.b * a.pool.Hkv;
+      w.it.seq = items.sequence(w.it.b);
+      w.it.P = w.it.seq.n * items.G;
+      w.it.p0 = (unit - pair * tiles) * a.plan.rows;
+      w.it.start = w.lo = 0;
+      w.it.end = w.hi = w.q = 1;
+      w.more = w.it.p0 < w.it.P;
+    } else {
+      const Items::Scan first = items.scan(0);
+      const int64_t N = items.total(first);
+      w.q = max((int64_t)((double)N * a.plan.inv_units) + 1, (int64_t)a.plan.step * items.G);
+      w.lo = unit * w.q;
+      w.hi = min(w.lo + w.q, N);
+      w.more = w.lo < w.hi;
+      if (w.more) w.it = items.find(w.lo, first);
     }
-    if (threadIdx.x == 64 * WAVES - 1) a.cuts[unit] = cut;
-    if (lo >= hi) return;
+    walk = w;
   }
   for (int slot = 0;; slot = 1) {
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __syncthreads();
+    const bool more = __builtin_amdgcn_readfirstlane(walk.more) != 0;
+    const int64_t start = scalar64(walk.it.start), end = scalar64(walk.it.end);
+    const int64_t lo = scalar64(walk.lo), hi = scalar64(walk.hi);
+    if (tiles == 0 && slot == 0 && wave == WAVES - 1) {   // (the wave with the fewest steps)
+      // does this unit hold its first item's first cut?
+      PageCut cut = {0, -1, 0, 0, 0, 0, 0, 0};
+      const int64_t q = scalar64(walk.q);
+      if (more && start < lo && start >= lo - q)
+        cut = PageCut{unit - 1, (int)over64(end - 1, q), start == lo - q ? 0 : 1, walk.it.kv, walk.it.seq.r0,
+                      walk.it.p0, walk.it.P, 0};
+      if ((threadIdx.x & 63) == 0) a.cuts[unit] = cut;
+    }
+    if (!more) return;
     {
-      const Walk &w = state[wave];
       Item it;
-      it.b = __builtin_amdgcn_readfirstlane(w.it.b);
-      it.kv = __builtin_amdgcn_readfirstlane(w.it.kv);
-      it.p0 = __builtin_amdgcn_readfirstlane(w.it.p0);
-      it.P = __builtin_amdgcn_readfirstlane(w.it.P);
-      it.seq.r0 = __builtin_amdgcn_readfirstlane(w.it.seq.r0);
-      it.seq.n = __builtin_amdgcn_readfirstlane(w.it.seq.n);
-      it.seq.len = __builtin_amdgcn_readfirstlane(w.it.seq.len);
-      const int64_t start = scalar64(w.it.start), lo = scalar64(w.lo), hi = scalar64(w.hi);
+      it.b = __builtin_amdgcn_readfirstlane(walk.it.b);
+      it.kv = __builtin_amdgcn_readfirstlane(walk.it.kv);
+      it.p0 = __builtin_amdgcn_readfirstlane(walk.it.p0);
+      it.P = __builtin_amdgcn_readfirstlane(walk.it.P);
+      it.seq.r0 = __builtin_amdgcn_readfirstlane(walk.it.seq.r0);
+      it.seq.n = __builtin_amdgcn_readfirstlane(walk.it.seq.n);
+      it.seq.len = __builtin_amdgcn_readfirstlane(walk.it.seq.len);
       // the keys its last row sees
       const int last = (min(it.p0 + a.plan.rows, it.P) - 1) / items.G;
-      const int end = max(0, it.seq.len - it.seq.n + last + 1);
+      const int seen = max(0, it.seq.len - it.seq.n + last + 1);
       auto key_at = [&](int64_t x) {
         const int64_t keys = (int64_t)((double)(x - start) * a.plan.inv_group);
-        return (int)min(keys & -(int64_t)a.plan.step, (int64_t)end);   // (a step is a power of two)
+        return (int)min(keys & -(int64_t)a.plan.step, (int64_t)seen);   // (a step is a power of two)
       };
-      const bool head = start >= lo, tail = scalar64(w.it.end) <= hi;
-      const int k0 = head ? 0 : key_at(lo), k1 = tail ? end : key_at(hi);
+      const bool head = start >= lo, tail = end <= hi;
+      const int k0 = head ? 0 : key_at(lo), k1 = tail ? seen : key_at(hi);
       body(it, __builtin_amdgcn_readfirstlane(k0), __builtin_amdgcn_readfirstlane(k1), head && tail, slot);
     }
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-    {
-      Item it = state[wave].it;
+    if (wave == 0) {
+      Item it = walk.it;
       it.start = scalar64(it.start);
       it.end = scalar64(it.end);
       it.p0 = __builtin_amdgcn_readfirstlane(it.p0);
+      it.P = __builtin_amdgcn_readfirstlane(it.P);
       if (tiles > 0) {                      // (more rows than the hint said)
         const int64_t p0 = it.p0 + (int64_t)tiles * a.plan.rows;
-        if (p0 >= __builtin_amdgcn_readfirstlane(it.P)) return;
-        state[wave].it.p0 = (int)p0;
-        continue;
+        walk.more = p0 < it.P;
+        walk.it.p0 = (int)p0;
+      } else if (it.end >= scalar64(walk.hi)) {
+        walk.more = 0;
+      } else {
+        it.b = __builtin_amdgcn_readfirstlane(it.b);
+        it.kv = __builtin_amdgcn_readfirstlane(it.kv);
+        it.seq.r0 = __builtin_amdgcn_readfirstlane(it.seq.r0);
+        it.seq.n = __builtin_amdgcn_readfirstlane(it.seq.n);
+        it.seq.len = __builtin_amdgcn_readfirstlane(it.seq.len);
+        walk.it = items.next(it);
       }
-      if (it.end >= scalar64(state[wave].hi)) return;
-      it.b = __builtin_amdgcn_readfirstlane(it.b);
-      it.kv = __builtin_amdgcn_readfirstlane(it.kv);
-      it.seq.r0 = __builtin_amdgcn_readfirstlane(it.seq.r0);
-      it.seq.n = __builtin_amdgcn_readfirstlane(it.seq.n);
-      it.seq.len = __builtin_amdgcn_readfirstlane(it.seq.len);
-      state[wave].it = items.next(it);
     }
   }
 }
@@ -303,6 +313,12 @@ __device__ __forceinline__ int xcd_remap(int i, int n) {
 //   goes from one MFMA to the next without leaving its lane, and V comes as four
 //   rows' pieces of d / 16 channels, again 16 bytes a lane and group (FP4, d 128).
 // Both loads of a group are one contiguous KiB of the page.
+//
+// Bound by HBM where there is much to read: 16 sequences of 9 K to 36 K tokens, 4 KV
+// heads of 128 in FP4, 195 MB: 47 us, of which the keys take 37 (5.3 TB/s), the start (cut,
+// tables, first loads) 4 and the joins 5.  28 layers of 2 K to 6 K tokens, 63 MB: 23 us, as
+// much start and join as keys; a dependent chain of loads, not traffic, bounds those.
+//
 // What a lane holds of a step's 32 keys, as it lies in the page: WK words of K and
 // WV of V for each group of 16 keys, and with FP4 the scales.
 template <int D, bool FP4>
@@ -334,7 +350,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void page_attn_few(PageAt
   using B = PageBlock<D, FP4>;
   constexpr int KK = D / 32;                // MFMAs of S for each group of keys
   constexpr int PC = D / 16;                // channels of a piece of V
-  constexpr int AHEAD = FP4 ? 2 : 1;        // steps in flight beside the one computed
+  // Steps in flight beside the one computed.  A step of bf16 at head size 128 is 64 registers
+  // a lane: with one more of them 32 rows spill (11 sequences, 8 rows of 32 + 8 heads: 80 us, 58
+  // without).
+  constexpr int AHEAD = FP4 ? 2 : D == 128 && RT == 2 ? 0 : 1;
   const PagePool &pool = a.pool;
   const int Hq = pool.Hq, G = Hq / pool.Hkv;
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
@@ -349,10 +368,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void page_attn_few(PageAt
   const int ks_ofs = B::ks(page_rows, n16) + u * (D / 4) / 32;
   const int vs_ofs = B::vs(page_rows, u) + n16 * PC / 32 * 4;
 
-  // the waves' states, in two buffers: a wave may leave its next one while others still read
-  __shared__ __attribute__((aligned(16))) float so_[2][NW][16][D + 4];
-  __shared__ float2 sml_[2][NW][16];
-  int joins = 0;
+  // the waves' states of 16 rows (32 rows: in two buffers, so that a wave may leave its second
+  // ones while others still read the first)
+  __shared__ __attribute__((aligned(16))) float so_[RT][NW][16][D + 4];
+  __shared__ float2 sml_[RT][NW][16];
 
   walk_items<NW>(a, unit, [&](const Item &it, int lo, int hi, bool whole, int slot) {
     // keys [lo, hi); row i of the sequence sees those below base + i + 1
@@ -565,9 +584,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void page_attn_few(PageAt
       float l = l_run[t];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      float(*so)[16][D + 4] = so_[joins & 1];
-      float2(*sml)[16] = sml_[joins & 1];
-      ++joins;
+      float(*so)[16][D + 4] = so_[t];
+      float2(*sml)[16] = sml_[t];
       if (u == 0) sml[wave][n16] = float2{m_run[t], l};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -995,8 +1013,9 @@ __global__ __launch_bounds__(MT, 1) void page_attn_many(PageAttnArgs a) {
 // first cut when items are long, so every workgroup adds up all cuts' tasks and takes
 // every gridDim.x-th (with a workgroup for each (unit, 64 float4), 64 rows on 8192 tokens
 // took 34 us here, most of it workgroups that found nothing to do).
-constexpr int kJoinUnits = 512;         // units of a launch at most
+constexpr int kJoinUnits = kStreamSlots;   // units of a launch with cuts at most: a thread a unit
 constexpr int kFewParts = 4;
+static_assert(kJoinUnits == 256, "a thread a unit");
 
 template <int D, bool MANY>
 __global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
@@ -1011,19 +1030,13 @@ __global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
     const int n = min(rows, c.P - c.p0);
     return MANY ? (n + 31) / 32 * (D / 8) : (n * (D / 4) + 63) / 64;
   };
-  // thread t has the cuts 2 t and 2 t + 1
-  int n[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int i = 2 * threadIdx.x + x;
-    n[x] = 0;
-    if (i < a.plan.units) {
-      const PageCut c = a.cuts[i];
-      const int parts = c.last - c.first + 1;
-      if (parts > 0) n[x] = parts > kFewParts ? groups(c) : (groups(c) + 3) / 4;
-    }
+  int n = 0;
+  if ((int)threadIdx.x < a.plan.units) {
+    const PageCut c = a.cuts[threadIdx.x];
+    const int parts = c.last - c.first + 1;
+    if (parts > 0) n = parts > kFewParts ? groups(c) : (groups(c) + 3) / 4;
   }
-  const int64_t sums = wave_sums(n[0] + n[1]);
+  const int64_t sums = wave_sums(n);
   if (lane == 63) wsum[wave] = (int)sums;
   __syncthreads();
   int before = 0, total = 0;
@@ -1032,8 +1045,7 @@ __global__ __launch_bounds__(256) void page_combine(PageAttnArgs a) {
     before += w < wave ? wsum[w] : 0;
     total += wsum[w];
   }
-  upto[2 * threadIdx.x + 1] = before + (int)sums;
-  upto[2 * threadIdx.x] = before + (int)sums - n[1];
+  upto[threadIdx.x] = before + (int)sums;
   __syncthreads();
 
   for (int task = blockIdx.x; task < total; task += gridDim.x) {
@@ -1142,7 +1154,7 @@ hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   else hipLaunchKernelGGL((page_attn_many<D, FP4, 8>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan.tiles > 0) return e;
-  const dim3 joins(2 * kJoinUnits);
+  const dim3 joins(4 * kStreamSlots);
   if (rows <= 32) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);
   return hipGetLastError();

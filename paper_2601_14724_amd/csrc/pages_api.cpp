@@ -28,10 +28,10 @@ int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
   if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
   if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;
   if ((int64_t)b->n_rows * (p->n_q_heads / p->n_kv_heads) > 1 << 30) return HERMES_EINVAL;
-  // the cost of all items of an attention call has to fit 62 bits (items of 16 rows, one more a pair)
+  // the cost of all items of an attention call has to be exact as a double (items of 16 rows, one more a pair)
   const double G = (double)p->n_q_heads / p->n_kv_heads, keys = (double)b->max_pages * p->page_rows;
   const double items = (double)b->n_rows * p->n_q_heads / 16.0 + (double)b->n_seqs * p->n_kv_heads;
-  if (items * (G * (keys + 1024.0) + (double)b->n_rows * G) > 4.0e18) return HERMES_EINVAL;
+  if (items * (G * (keys + 1024.0) + (double)b->n_rows * G) > 4.0e15) return HERMES_EINVAL;
   return HERMES_OK;
 }
 
@@ -124,6 +124,7 @@ int check_page_pool(const hermes_page_pool *p) {
   if (p->page_rows < 16 || p->page_rows > 256 || (p->page_rows & (p->page_rows - 1)) != 0) return HERMES_EINVAL;
   if (p->n_pages < 1) return HERMES_EINVAL;
   if (!std::isfinite(p->sm_scale) || !std::isfinite(p->rope_theta)) return HERMES_EINVAL;
+  if (p->sm_scale > 0.0 && (p->sm_scale < 1e-30 || p->sm_scale > 1e30)) return HERMES_EINVAL;   // (an fp32 with an inverse)
   if (p->rope_axes != 0 && p->rope_axes != 1 && p->rope_axes != 3) return HERMES_EINVAL;
   if (p->rope_axes == 3) {
     const int *sec = p->mrope_section;

@@ -50,7 +50,7 @@ def _read(pool, batch, k=FAKE, v=FAKE):
 
 BAD_POOLS = [dict(n_kv_heads=0), dict(n_q_heads=5), dict(n_q_heads=1), dict(format=2), dict(format=-1),
              dict(page_rows=8), dict(page_rows=48), dict(page_rows=512), dict(n_pages=0), dict(pages=None),
-             dict(pages=FAKE + 8), dict(status=FAKE + 2), dict(sm_scale=float("inf")),
+             dict(pages=FAKE + 8), dict(status=FAKE + 2), dict(sm_scale=float("inf")), dict(sm_scale=1e-40), dict(sm_scale=1e39),
              dict(rope_theta=float("nan")), dict(rope_axes=2), dict(rope_axes=3, mrope_section=(1, 2, 3)),
              dict(rope_axes=3, mrope_section=(-1, 17, 16)), dict(n_q_heads=1 << 17, n_kv_heads=1)]
 BAD_BATCHES = [dict(n_seqs=-1), dict(n_rows=-1), dict(max_rows=-1), dict(max_len=-1), dict(max_pages=0),
