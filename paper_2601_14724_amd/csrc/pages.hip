@@ -281,7 +281,7 @@ constexpr int kAhead = 4;           // passes of q whose loads are on their way 
 template <int D, bool FP4>
 __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
   constexpr int HD = D / 2, CH = D / 8, HP = 64 / CH;    // pieces of a head, heads of a pass
-  __shared__ double2 trig[NT / 64][64];
+  __shared__ double2 trig[NT / 64][72];     // frequency f at f + f / 8: a wave reads every eighth at once
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int share = a.share, nth = wave % share;
   const int row = blockIdx.x * (NT / 64 / share) + wave / share;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
   const int q_passes = (Hq + HP - 1) / HP;
   const int piece = lane % CH, hl = lane / CH;
   const bool turn = a.rope != nullptr, second = piece >= CH / 2;
-  const int f0 = 8 * (piece % (CH / 2));
+  const int f0 = 9 * (piece % (CH / 2));    // (where the piece's eight frequencies lie)
   const uint16_t *q = a.q + (int64_t)row * a.q_stride;
   const uint16_t *k = a.k + (int64_t)row * a.k_stride, *v = a.v + (int64_t)row * a.v_stride;
 
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(NT) void page_append(PageAppendArgs a) {
   if (turn) {
     double sn, cs;
     sincos((double)pos * freq, &sn, &cs);
-    trig[wave][lane] = double2{cs, sn};
+    trig[wave][lane + lane / 8] = double2{cs, sn};
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
   }
   auto rotated = [&](const uint4 &x) {

@@ -252,6 +252,25 @@ def test_attend_scale_strides_and_rows_behind():
         assert (out[5:] == 3.0).all() and (lse[5:] == 3.0).all()
 
 
+@pytest.mark.parametrize("d,fmt", [(64, "fp4"), (128, "bf16")])
+def test_rows_before_the_first_start(d, fmt):
+    """row_start[0] > 0: the rows before it are no sequence's, and stay as they are."""
+    s = Setup((4, 2, d), fmt, 16, [3, 2], [40, 7], behind=7)
+    start = s.start + 4
+    batch = H.PageBatch(i32(s.tables), i32([40, 7]), i32(start), n_rows=s.n)
+    out = torch.full((s.n, 4, d), 3.0, dtype=torch.bfloat16, device=DEV)
+    kb, vb = (torch.full((s.n, 2, d), 3.0, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    s.pool.attend(batch, dev(s.q), out=out)
+    s.pool.read(batch, kb, vb)
+    for x in (out, kb, vb):
+        assert (x[:4] == 3.0).all() and (x[9:] == 3.0).all()
+    s.q = s.q[4:]
+    s.check_attend(out[4:], None)
+    for b, (r, t) in enumerate(zip(s.rows, s.lens)):
+        assert (f64(kb)[start[b]:start[b + 1]] == orc.stored(s.k[b], fmt)[t - r:]).all()
+    assert s.pool.faults() == 0
+
+
 def test_attend_long_split():
     """One token over a long sequence: many ranges, joined."""
     s = Setup((14, 2, 64), "fp4", 64, [1, 1], [20011, 1], seed=11).hints(1, 20011)
@@ -362,11 +381,12 @@ def test_two_streams_at_once():
         assert all(torch.equal(x, want[i]) for x in got[i])
 
 
-@pytest.mark.parametrize("fmt", ["fp4", "bf16"])
-def test_captured_decoding(fmt):
+@pytest.mark.parametrize("fmt,first", [("fp4", [30, 500, 1]), ("bf16", [30, 500, 1]), ("fp4", [9000, 4000, 1])])
+def test_captured_decoding(fmt, first):
     """A captured token (append, then attend) replayed while lengths, positions and inputs
-    move on, against the same calls made eagerly."""
-    steps, first = 5, [30, 500, 1]
+    move on, against the same calls made eagerly; short sequences without cuts, and long ones
+    with."""
+    steps = 5
     s = Setup((14, 2, 64), fmt, 16, [1] * 3, [t + steps for t in first], seed=22, fill=False)
     for b, t in enumerate(first):
         orc.store(s.pages, s.tables[b], s.k[b][:t], s.v[b][:t], 16, fmt)
@@ -376,7 +396,7 @@ def test_captured_decoding(fmt):
     ins = [[dev(orc.bf16_bits(rng.standard_normal((3, h, 64)))) for h in (14, 2, 2)] for _ in range(steps)]
     q, k, v = (x.clone() for x in ins[0])
     kv_len, rope, out = i32(first), i32(first), torch.empty_like(q)
-    batch = H.PageBatch(i32(s.tables), kv_len, max_len=600)
+    batch = H.PageBatch(i32(s.tables), kv_len, max_len=max(first) + steps)
     kv_len += 1
 
     def token(pool, batch):
