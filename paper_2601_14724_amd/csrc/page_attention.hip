@@ -1154,7 +1154,7 @@ hipError_t attend(const PageAttnArgs &a, hipStream_t s) {
   else hipLaunchKernelGGL((page_attn_many<D, FP4, 8>), grid, dim3(MT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan.tiles > 0) return e;
-  const dim3 joins(4 * kStreamSlots);
+  const dim3 joins(8 * kStreamSlots);
   if (rows <= 32) hipLaunchKernelGGL((page_combine<D, false>), joins, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((page_combine<D, true>), joins, dim3(256), 0, s, a);
   return hipGetLastError();
