@@ -484,7 +484,7 @@ typedef struct {
  * tokens: with n of them, row i is token kv_len[b] - n + i.  Token t lives in row
  * t % page_rows of page tables[b][t / page_rows].
  *  n_seqs       sequences (0 is allowed: the call does nothing).
- *  n_rows       rows of the stacked inputs; rows that belong to no sequence
+ *  n_rows       rows of the stacked inputs, 2^25 at most; rows that belong to no sequence
  *               (before row_start[0], from row_start[n_seqs] on) are neither read nor
  *               written.
  *  max_rows     most rows of a sequence, and max_len the greatest length (0: n_rows,

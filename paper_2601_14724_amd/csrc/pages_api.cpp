@@ -23,7 +23,8 @@ int64_t block_bytes(const hermes_page_pool *p) {
 
 int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
   if (b == nullptr || b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_len < 0) return HERMES_EINVAL;
-  if (b->n_rows > 1 << 30 || (b->row_start == nullptr && b->n_rows != b->n_seqs)) return HERMES_EINVAL;
+  // (a row a wave: a launch's threads have to stay below 2^32)
+  if (b->n_rows > 1 << 25 || (b->row_start == nullptr && b->n_rows != b->n_seqs)) return HERMES_EINVAL;
   if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
   if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
   if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;

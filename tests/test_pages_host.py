@@ -71,6 +71,15 @@ def test_bad_batches_are_refused(over):
         assert call(_pool(), _batch(**over)) == H.EINVAL
 
 
+def test_more_rows_than_a_launch_holds_are_refused():
+    """A row takes a wave, and a launch's threads are counted in 32 bits: 2^26 rows are 2^32."""
+    for call in (_append, _attend, _read):
+        assert call(_pool(), _batch(n_rows=1 << 26)) == H.EINVAL
+        assert call(_pool(), _batch(n_rows=(1 << 25) + 1)) == H.EINVAL
+    most = _batch(n_rows=1 << 25, max_rows=0, max_len=0)     # (no hints, so that cuts are planned for)
+    assert H.lib.hermes_page_workspace_bytes(ctypes.byref(_pool()), ctypes.byref(most)) > 0
+
+
 def test_null_structs_and_head_dims_are_refused():
     for call in (_append, _attend, _read):
         assert call(None, _batch()) == H.EINVAL
