@@ -477,6 +477,9 @@ class PageBatch:
                 raise ValueError("n_rows: needed with row_start")
         elif n_rows not in (None, n):
             raise ValueError("n_rows: one row a sequence without row_start")
+        for t in (tables, row_start):     # (a call compares the device of kv_len with its pool's)
+            if t is not None and t.device != kv_len.device:
+                raise ValueError(f"tables, kv_len and row_start: one device, got {t.device} and {kv_len.device}")
         self.tables, self.kv_len, self.row_start = tables, kv_len, row_start
         self.n_seqs, self.n_rows = n, n if n_rows is None else int(n_rows)
         b = PageBatchStruct()

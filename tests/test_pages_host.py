@@ -5,6 +5,7 @@ import itertools
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import pages_oracle as orc
 from paper_2601_14724_amd import hermes as H
@@ -106,6 +107,17 @@ def test_bad_attend_and_read_arguments_are_refused():
     need = H.lib.hermes_page_workspace_bytes(ctypes.byref(p), ctypes.byref(b))
     assert need > 0 and _attend(p, b, nbytes=need - 1) == H.ECAPACITY
     assert _read(p, b, k=FAKE + 8) == H.EINVAL and _read(p, b, v=FAKE + 2) == H.EINVAL
+
+
+def test_a_batch_on_two_devices_is_refused(monkeypatch):
+    """(shapes and types are checked elsewhere; the "meta" device stands in for a second one)"""
+    monkeypatch.setattr(H, "_need", lambda *a: None)
+    here, there = [lambda *s, d=d: torch.empty(s, dtype=torch.int32, device=d) for d in ("cpu", "meta")]
+    H.PageBatch(here(3, 8), here(3), here(4), n_rows=5)
+    for tables, lens, starts in ((there(3, 8), here(3), here(4)), (here(3, 8), there(3), here(4)),
+                                 (here(3, 8), here(3), there(4))):
+        with pytest.raises(ValueError, match="device"):
+            H.PageBatch(tables, lens, starts, n_rows=5)
 
 
 def test_empty_batches_do_nothing():
