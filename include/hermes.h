@@ -449,7 +449,9 @@ enum {
                                   stored, and read as zeros                           */
   HERMES_PAGE_BAD_LENGTH = 2,  /* a length below 0 or beyond the sequence's table: the
                                   sequence counts as empty                            */
-  HERMES_PAGE_BAD_ROWS = 4     /* row starts that fall, or leave 0 .. n_rows: clamped  */
+  HERMES_PAGE_BAD_ROWS = 4     /* row starts that fall, or leave 0 .. n_rows: clamped (a
+                                  row that two sequences then hold gets the results of
+                                  one of them)                                        */
 };
 
 /*

@@ -110,29 +110,50 @@ struct Items {
   int G;
   __device__ __forceinline__ Items(const PageAttnArgs &a)
       : pool(a.pool), seqs(a.seqs), plan(a.plan), G(a.pool.Hq / a.pool.Hkv) {}
-  // Lane l has sequence b0 + l: its bounds, and the sum of the costs up to it.
+  // Lane l has sequence b0 + l: its bounds, and the sum of the costs up to it.  A start that
+  // falls counts as the greatest before it, so that no two sequences share rows: the host has
+  // bounded the cost of n_rows rows, and starts on the device could ask for those of every
+  // sequence.  from: the row where the sequences before b0 end.
   struct Scan {
     PageSeq seq;
     int64_t sums;
   };
-  __device__ __forceinline__ Scan scan(int b0) const {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ Scan scan(int b0, int from) const {
+    const int lane = threadIdx.x & 63, b = b0 + lane;
+    const bool on = b < seqs.n_seqs, starts = on && seqs.row_start != nullptr;
+    int a0 = starts ? seqs.row_start[b] : b, a1 = starts ? seqs.row_start[b + 1] : b + 1;
+    const int len = on ? seqs.kv_len[b] : 0;
+    if (__builtin_expect(__any(starts && (a1 < a0 || a0 < from)), 0)) {
+      page_note(pool, HERMES_PAGE_BAD_ROWS);
+      a1 = max(max(a0, a1), from);
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) a1 = max(a1, __shfl_up(a1, d));
+      const int before = __shfl_up(a1, 1);
+      a0 = lane > 0 ? before : max(a0, from);
+    }
     Scan x = {{0, 0, 0}, 0};
-    if (b0 + lane < seqs.n_seqs) {
-      x.seq = page_seq(pool, seqs, b0 + lane);
+    if (on) {
+      x.seq = page_seq_of(pool, seqs, a0, a1, len);
       const SeqCost c(x.seq, G, plan);
       x.sums = pool.Hkv * c.sum(c.items);
     }
     x.sums = wave_sums(x.sums);
     return x;
   }
-  // the cost of all; first: scan(0)
-  __device__ __forceinline__ int64_t total(const Scan &first) const {
-    int64_t n = lane64(first.sums, 63);
-    for (int b = 64; b < seqs.n_seqs; b += 64) n += lane64(scan(b).sums, 63);
+  // the row where the 64 sequences of a scan end (more follow)
+  __device__ __forceinline__ int end_of(const Scan &s) const {
+    return __builtin_amdgcn_readlane(s.seq.r0 + s.seq.n, 63);
+  }
+  // the cost of all; s: scan(0, 0)
+  __device__ __forceinline__ int64_t total(Scan s) const {
+    int64_t n = lane64(s.sums, 63);
+    for (int b = 64; b < seqs.n_seqs; b += 64) {
+      s = scan(b, end_of(s));
+      n += lane64(s.sums, 63);
+    }
     return n;
   }
-  // The item that holds x (x < total); s: scan(0).
+  // The item that holds x (x < total); s: scan(0, 0).
   __device__ __forceinline__ Item find(int64_t x, Scan s) const {
     int64_t before = 0;
     int b = 0, l;
@@ -142,15 +163,23 @@ struct Items {
       if (past != 0ull || b + 64 >= seqs.n_seqs) break;
       before += lane64(s.sums, 63);
       b += 64;
-      s = scan(b);
+      s = scan(b, end_of(s));
     }
     before += l > 0 ? lane64(s.sums, l - 1) : 0;
     const PageSeq seq = {__builtin_amdgcn_readlane(s.seq.r0, l), __builtin_amdgcn_readlane(s.seq.n, l),
                          __builtin_amdgcn_readlane(s.seq.len, l)};
     return in_sequence(b + l, seq, before, x);
   }
-  __device__ __forceinline__ PageSeq sequence(int b) const {
-    const PageSeq s = page_seq(pool, seqs, b);
+  // Sequence b; from: the row where the one before ends.
+  __device__ __forceinline__ PageSeq sequence(int b, int from) const {
+    const bool starts = seqs.row_start != nullptr;
+    int a0 = starts ? seqs.row_start[b] : b, a1 = starts ? seqs.row_start[b + 1] : b + 1;
+    if (a0 < from || a1 < a0) {
+      page_note(pool, HERMES_PAGE_BAD_ROWS);
+      a0 = max(a0, from);
+      a1 = max(a0, a1);
+    }
+    const PageSeq s = page_seq_of(pool, seqs, a0, a1, seqs.kv_len[b]);
     return {__builtin_amdgcn_readfirstlane(s.r0), __builtin_amdgcn_readfirstlane(s.n),
             __builtin_amdgcn_readfirstlane(s.len)};
   }
@@ -188,8 +217,8 @@ struct Items {
     const int64_t before = it.start - it.kv * head - c.sum(it.p0 / plan.rows);
     if (it.end < before + all) return in_sequence(it.b, it.seq, before, it.end);
     int b = it.b + 1;                      // (sequences without rows have no items)
-    PageSeq seq = sequence(b);
-    while (b + 1 < seqs.n_seqs && seq.n == 0) seq = sequence(++b);
+    PageSeq seq = sequence(b, it.seq.r0 + it.seq.n);
+    while (b + 1 < seqs.n_seqs && seq.n == 0) seq = sequence(++b, seq.r0);
     return in_sequence(b, seq, it.end, it.end);
   }
 };
@@ -216,14 +245,14 @@ __device__ __forceinline__ void walk_items(const PageAttnArgs &a, int unit, F &&
       const int pair = unit / tiles;
       w.it.b = pair / a.pool.Hkv;
       w.it.kv = pair - w.it.b * a.pool.Hkv;
-      w.it.seq = items.sequence(w.it.b);
+      w.it.seq = items.sequence(w.it.b, 0);   // (starts that fall: two pairs may write one row)
       w.it.P = w.it.seq.n * items.G;
       w.it.p0 = (unit - pair * tiles) * a.plan.rows;
       w.it.start = w.lo = 0;
       w.it.end = w.hi = w.q = 1;
       w.more = w.it.p0 < w.it.P;
     } else {
-      const Items::Scan first = items.scan(0);
+      const Items::Scan first = items.scan(0, 0);
       const int64_t N = items.total(first);
       w.q = max((int64_t)((double)N * a.plan.inv_units) + 1, (int64_t)a.plan.step * items.G);
       w.lo = unit * w.q;
