@@ -485,7 +485,8 @@ typedef struct {
  * row_start[b] .. row_start[b + 1] - 1 belong to sequence b and are its last
  * tokens: with n of them, row i is token kv_len[b] - n + i.  Token t lives in row
  * t % page_rows of page tables[b][t / page_rows].
- *  n_seqs       sequences (0 is allowed: the call does nothing).
+ *  n_seqs       sequences (0 is allowed: the call does nothing), n_seqs x n_kv_heads 2^24 at
+ *               most.
  *  n_rows       rows of the stacked inputs, 2^25 at most; rows that belong to no sequence
  *               (before row_start[0], from row_start[n_seqs] on) are neither read nor
  *               written.
@@ -493,6 +494,7 @@ typedef struct {
  *               and what the tables hold).  They only choose how the work is cut:
  *               longer sequences are handled all the same, slower.
  *  max_pages    entries of a table; those past a sequence's last token are not read.
+ *               max_pages x page_rows is 2^31 - 257 at most.
  *  row_start    device int32 [n_seqs + 1], not falling; NULL: one row a sequence
  *               (n_rows = n_seqs).
  *  kv_len       device int32 [n_seqs]: lengths, the call's own rows among them.
@@ -552,6 +554,9 @@ size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_pa
  *               NULL if that is 0); free again when the call's work is done.
  * A row that sees no token gets zeros, and -infinity in lse.  Stored values are
  * taken to be finite, as q is.
+ * With G = n_q_heads / n_kv_heads and T = max_pages x page_rows,
+ * (n_rows x n_q_heads / 16 + n_seqs x n_kv_heads) x G x (T + 1024 + n_rows) is 4 x 10^15
+ * at most (the work is cut by sums of this size).
  * Errors: EINVAL, ENOTSUP, ECAPACITY (workspace too small), EHIP.
  */
 int hermes_page_attend(const hermes_page_pool *pool, const hermes_page_batch *batch, const void *q,

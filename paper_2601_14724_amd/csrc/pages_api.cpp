@@ -28,8 +28,13 @@ int check_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
   if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
   if (b->max_pages < 1 || (int64_t)b->max_pages * p->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
   if ((int64_t)b->n_seqs * p->n_kv_heads > 1 << 24) return HERMES_EINVAL;
-  if ((int64_t)b->n_rows * (p->n_q_heads / p->n_kv_heads) > 1 << 30) return HERMES_EINVAL;
-  // the cost of all items of an attention call has to be exact as a double (items of 16 rows, one more a pair)
+  return HERMES_OK;
+}
+
+// What an attention call asks of a (good) batch beside that: the cost of all items has to
+// be exact as a double (items of 16 rows, one more a pair; it keeps n_rows G below 2^28).
+int check_attend_batch(const hermes_page_pool *p, const hermes_page_batch *b) {
+  if (b->n_seqs == 0 || b->n_rows == 0) return HERMES_OK;
   const double G = (double)p->n_q_heads / p->n_kv_heads, keys = (double)b->max_pages * p->page_rows;
   const double items = (double)b->n_rows * p->n_q_heads / 16.0 + (double)b->n_seqs * p->n_kv_heads;
   if (items * (G * (keys + 1024.0) + (double)b->n_rows * G) > 4.0e15) return HERMES_EINVAL;
@@ -168,6 +173,7 @@ size_t hermes_page_bytes(const hermes_page_pool *pool) {
 
 size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_page_batch *batch) {
   if (check_page_pool(pool) != HERMES_OK || check_batch(pool, batch) != HERMES_OK) return 0;
+  if (check_attend_batch(pool, batch) != HERMES_OK) return 0;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return 0;
   return workspace_of(pool, plan_of(pool, batch));
 }
@@ -209,6 +215,7 @@ int hermes_page_attend(const hermes_page_pool *pool, const hermes_page_batch *ba
                        int64_t q_stride, void *out, float *lse, void *workspace, size_t ws_bytes, void *stream) {
   int rc = check_page_memory(pool);
   if (rc == HERMES_OK) rc = check_batch(pool, batch);
+  if (rc == HERMES_OK) rc = check_attend_batch(pool, batch);
   if (rc != HERMES_OK) return rc;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return HERMES_OK;
   if ((rc = check_batch_memory(batch)) != HERMES_OK) return rc;

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2601_14724_amd import hermes as H
-from test_gpu_pages import DEV, Setup, dev, i32
+from oracle import pages_oracle as orc
+from test_gpu_pages import DEV, Setup, bits, dev, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +26,20 @@ def test_starts_that_fall_give_a_row_to_one_sequence(heads, fmt):
     lse = torch.empty((s.n, s.hq), device=DEV)
     s.check_attend(s.pool.attend(batch, dev(s.q), lse=lse), lse)
     assert s.pool.faults() == H.PAGE_BAD_ROWS
+
+
+def test_rows_are_stored_where_there_are_too_many_to_attend():
+    """2^14 + 1 rows of one KV head with 2^16 query heads: stored and read back, refused by attend."""
+    n, page = (1 << 14) + 1, 256
+    pool = H.KVPages(1 << 16, 1, 64, 65, page_rows=page, fmt=H.PAGE_BF16)
+    batch = H.PageBatch(i32(np.arange(65)[None]), i32([n]), i32([0, n]), n_rows=n)
+    rng = np.random.default_rng(32)
+    k, v = (orc.bf16_bits(rng.standard_normal((n, 1, 64))) for _ in "kv")
+    pool.append(batch, dev(k), dev(v))
+    kb, vb = pool.read(batch)
+    assert (bits(kb) == k).all() and (bits(vb) == v).all()
+    none = torch.empty(1, dtype=torch.bfloat16, device=DEV)     # (never read)
+    with pytest.raises(H.HermesError) as e:
+        pool._run(H.lib.hermes_page_attend, "hermes_page_attend", pool._ref, batch._ref, none.data_ptr(), 1 << 22,
+                  none.data_ptr(), None, None, 0)
+    assert e.value.code == H.EINVAL
