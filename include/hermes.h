@@ -490,9 +490,10 @@ typedef struct {
  *  n_rows       rows of the stacked inputs, 2^25 at most; rows that belong to no sequence
  *               (before row_start[0], from row_start[n_seqs] on) are neither read nor
  *               written.
- *  max_rows     most rows of a sequence, and max_len the greatest length (0: n_rows,
- *               and what the tables hold).  They only choose how the work is cut:
- *               longer sequences are handled all the same, slower.
+ *  max_rows     most rows of a sequence (0: n_rows; without row_start it is one, whatever
+ *               is given here), and max_len the greatest length (0: what the tables
+ *               hold).  They only choose how the work is cut: longer sequences are
+ *               handled all the same, slower.
  *  max_pages    entries of a table; those past a sequence's last token are not read.
  *               max_pages x page_rows is 2^31 - 257 at most.
  *  row_start    device int32 [n_seqs + 1], not falling; NULL: one row a sequence

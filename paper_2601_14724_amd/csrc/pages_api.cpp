@@ -63,7 +63,7 @@ constexpr int kWholeSteps = 16;   // steps of a round's longest items without cu
 // The cut of an attention call, from what the host knows of it.
 PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
-  const int64_t max_rows = b->max_rows > 0 && b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
+  const int64_t max_rows = b->row_start == nullptr ? 1 : b->max_rows > 0 && b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
   const int64_t table = (int64_t)b->max_pages * p->page_rows;
   const int64_t max_len = b->max_len > 0 && b->max_len < table ? b->max_len : table;
   const int64_t P = max_rows * G;

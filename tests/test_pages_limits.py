@@ -31,3 +31,13 @@ def test_the_cost_limit_is_the_headers():
             b = _batch(n_seqs=5, n_rows=n_rows, max_pages=max_pages, max_rows=0, max_len=0)
             cost = (n_rows * 28 / 16 + 5 * 4) * 7 * (max_pages * 32 + 1024 + n_rows)
             assert (_bytes(pool, b) > 0) == (cost <= 4e15), (n_rows, max_pages)
+
+
+def test_a_row_a_sequence_needs_no_hint():
+    """Without row starts every sequence has one row, whatever max_rows says."""
+    pool = _pool(n_q_heads=28, n_kv_heads=4, head_dim=128)
+    for seqs in (1, 3, 28, 256):
+        for pages in (1, 20, 300):
+            got = {_bytes(pool, _batch(n_seqs=seqs, n_rows=seqs, row_start=None, max_rows=m, max_len=0, max_pages=pages))
+                   for m in (0, 1, 2, seqs, 1000)}
+            assert len(got) == 1, (seqs, pages, got)
