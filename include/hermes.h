@@ -500,8 +500,9 @@ typedef struct {
  *               (n_rows = n_seqs).
  *  kv_len       device int32 [n_seqs]: lengths, the call's own rows among them.
  *  tables       device int32 [n_seqs][max_pages]: page ids.  Sequences may share
- *               pages that no call writes; of rows that are stored twice in one call,
- *               either may stay.
+ *               pages that no call writes.  Where one call stores two rows in one place,
+ *               what is there afterwards is not defined (rows are stored in pieces, codes
+ *               apart from scales, so it may be parts of both).
  */
 typedef struct {
   int32_t n_seqs;
