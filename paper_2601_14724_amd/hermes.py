@@ -508,8 +508,10 @@ class KVPages:
         for i in range(3):
             p.mrope_section[i] = int(mrope_section[i])
         self.page_bytes = lib.hermes_page_bytes(ctypes.byref(p))
-        if self.page_bytes == 0:
-            raise HermesError(EINVAL, "hermes_page_bytes")
+        if self.page_bytes == 0:              # (why: a call of no rows looks at the pool alone)
+            p.pages = 16
+            raise HermesError(lib.hermes_page_read(ctypes.byref(p), ctypes.byref(PageBatchStruct()), None, None, None),
+                              "hermes_page_bytes")
         self.Hq, self.Hkv, self.d, self.axes = n_q_heads, n_kv_heads, head_dim, 3 if rope_axes == 3 else 1
         if pages is None:
             pages = torch.empty((n_pages, self.page_bytes), dtype=torch.uint8, device=device)

@@ -2,6 +2,8 @@
 on the host (no device)."""
 import ctypes
 
+import pytest
+
 from paper_2601_14724_amd import hermes as H
 from test_pages_host import _attend, _batch, _pool, _read
 
@@ -41,3 +43,12 @@ def test_a_row_a_sequence_needs_no_hint():
             got = {_bytes(pool, _batch(n_seqs=seqs, n_rows=seqs, row_start=None, max_rows=m, max_len=0, max_pages=pages))
                    for m in (0, 1, 2, seqs, 1000)}
             assert len(got) == 1, (seqs, pages, got)
+
+
+@pytest.mark.parametrize("over,code", [(dict(head_dim=96), H.ENOTSUP), (dict(head_dim=256), H.ENOTSUP), (dict(page_rows=24), H.EINVAL),
+                                       (dict(n_kv_heads=3), H.EINVAL), (dict(fmt=2), H.EINVAL), (dict(n_pages=0), H.EINVAL),
+                                       (dict(sm_scale=1e-40), H.EINVAL)], ids=str)
+def test_the_binding_says_why_a_pool_is_refused(over, code):
+    with pytest.raises(H.HermesError) as e:
+        H.KVPages(**(dict(n_q_heads=4, n_kv_heads=2, head_dim=64, n_pages=3) | over))
+    assert e.value.code == code
