@@ -78,11 +78,12 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   // keys where there are items enough (256 sequences of 1000 tokens, 4 KV heads: 38 us, 50
   // with eight).  A step is 32 keys for each wave, or a tile for each key group.
   const bool few = x.rows <= 32;
-  const int64_t tiles = over(P, x.rows), items = (int64_t)b->n_seqs * p->n_kv_heads * tiles;
+  const int64_t tiles = over(P, x.rows), all = (int64_t)b->n_seqs * p->n_kv_heads * tiles;
+  const int64_t items = all < 1 << 24 ? all : 1 << 24;   // (as good as more: cut, and products below 2^63)
   const bool four = few && items >= 2 * kStreamSlots;
   const int64_t slots = four ? 2 * kStreamSlots : kStreamSlots, step = few ? 256 : x.rows <= 128 ? 128 : 64;
   const int64_t longest = over(items, slots) * max_len * (four ? 2 : 1), shared = over(items * max_len, kStreamSlots);
-  if (longest <= kWholeSteps * step && longest - shared <= (few ? 8 : 4) * step && items <= 1 << 24) {
+  if (longest <= kWholeSteps * step && longest - shared <= (few ? 8 : 4) * step) {
     x.step = (int32_t)(four ? step / 2 : step);
     x.tiles = (int32_t)tiles;
     x.units = (int32_t)items;

@@ -12,10 +12,10 @@ HERE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "cpu_waves")
 CLANG = os.path.join(os.path.dirname(os.path.realpath(build.HIPCC)), "..", "llvm", "bin", "clang++")
 
 
-def compiled(tmp_path_factory, name):
+def compiled(tmp_path_factory, name, *options):
     exe = str(tmp_path_factory.mktemp("cpu_waves") / name)
     subprocess.run([CLANG, "-std=c++20", "-w", "-pthread", "-D__HIP__", f"-I{HERE}", f"-I{build.CSRC}",
-                    f"-I{build.INCLUDE}", os.path.join(HERE, name + ".cpp"), "-o", exe], check=True, timeout=120)
+                    f"-I{build.INCLUDE}", *options, os.path.join(HERE, name + ".cpp"), "-o", exe], check=True, timeout=120)
     return exe
 
 
@@ -48,3 +48,10 @@ def test_starts_that_fall_stay_in_bounds(walk_items, seqs, rows, heads, length, 
     res = subprocess.run([walk_items] + [str(x) for x in (seqs, rows, heads, length, ends)], capture_output=True, text=True,
                          timeout=100)
     assert res.returncode == 0 and res.stdout == f"in bounds, status {H.PAGE_BAD_ROWS}\n"
+
+
+def test_plans_of_any_size_are_counted_without_overflow(tmp_path_factory):
+    exe = compiled(tmp_path_factory, "plans", "-O1", "-fsanitize=signed-integer-overflow,float-cast-overflow",
+                   "-fno-sanitize-recover=all")
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert res.returncode == 0 and res.stdout == "good, many taken\n", res.stderr
