@@ -555,7 +555,8 @@ size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_pa
  *  workspace    device memory of hermes_page_workspace_bytes, 16-byte aligned (may be
  *               NULL if that is 0); free again when the call's work is done.
  * A row that sees no token gets zeros, and -infinity in lse.  Stored values are
- * taken to be finite, as q is.
+ * taken to be finite, as q is.  Scores, their maximum and sum, and the products' sums are
+ * fp32; a probability is rounded to bf16 before it meets the value.
  * With G = n_q_heads / n_kv_heads and T = max_pages x page_rows,
  * (n_rows x n_q_heads / 16 + n_seqs x n_kv_heads) x G x (T + 1024 + n_rows) is 4 x 10^15
  * at most (the work is cut by sums of this size).

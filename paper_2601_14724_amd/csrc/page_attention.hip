@@ -5,7 +5,11 @@
 // page_combine     joins the parts of items that were cut
 //
 // S = scale q k^T over the keys a row sees, O = softmax(S) V, in one pass over the
-// keys with a running maximum and sum (fp32), lse = ln sum exp S.
+// keys with a running maximum and sum (fp32), lse = ln sum exp S.  P = 2^(S - max) is
+// rounded to bf16 for the second product, whose other operand is V in bf16 (its sum is
+// not): each p off by 2^-8 of itself at most, which takes O's error in the 2-norm from
+// 1.7e-3 (O's own rounding to bf16) to 1.9e-3 to 2.4e-3.  P as a sum of two bf16 numbers
+// would double that product.
 //
 // The cut.  Lengths and rows are on the device and ragged, so the cut is made there:
 // every workgroup (unit) adds up the items' costs and takes an equal run of them,
@@ -344,8 +348,8 @@ __device__ __forceinline__ int xcd_remap(int i, int n) {
 // Both loads of a group are one contiguous KiB of the page.
 //
 // Bound by HBM where there is much to read: 16 sequences of 9 K to 36 K tokens, 4 KV
-// heads of 128 in FP4, 195 MB: 47 us, of which the keys take 37 (5.3 TB/s), the start (cut,
-// tables, first loads) 4 and the joins 5.  28 layers of 2 K to 6 K tokens, 63 MB: 23 us, as
+// heads of 128 in FP4, 195 MB: 47 us, of which the keys take about 39 (5 TB/s), the start (cut,
+// tables, first loads) 4 and the joins 4.5.  28 layers of 2 K to 6 K tokens, 63 MB: 23.6 us, as
 // much start and join as keys; a dependent chain of loads, not traffic, bounds those.
 //
 // What a lane holds of a step's 32 keys, as it lies in the page: WK words of K and
@@ -675,6 +679,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void page_attn_few(PageAt
 // and reads all of the tile from there, K row by row and V transposed by
 // ds_read_b64_tr_b16.  As in attn_fwd, S^T = K Q^T puts one query row a lane, so the softmax
 // stays in the lane and P^T is the B operand of O^T = V^T P^T as it is.
+//
+// Bound by the issue port and the chain S -> softmax -> P V (matrix units busy 44% by counters):
+// 3136 rows of 28 + 4 heads of 128 on 35904 tokens in FP4 take 1431 us with the joins (1.08
+// PFLOP/s), 64 rows on each of 28 layers' 4 K to 16 K tokens 304 us.
 constexpr int MT = 512, MW = MT / 64;   // waves
 constexpr int KPAD = 8, VPAD = 32;      // u16 padding of K and V rows in LDS
 

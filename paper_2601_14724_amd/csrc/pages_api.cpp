@@ -69,14 +69,21 @@ PagePlan plan_of(const hermes_page_pool *p, const hermes_page_batch *b) {
   const int64_t P = max_rows * G;
   PagePlan x;
   x.rows = P <= 16 ? 16 : P <= 32 ? 32 : P <= 64 ? 64 : P <= 128 ? 128 : 256;
+  // (0 / half / this / twice, us: 40 ragged sequences of 64 rows 243 / 123 / 110 / 119; one row of
+  // 64 sequences to 9 K tokens, FP4 200 / 94 / 75 / 79; of 11 to 10 K, bf16 71 / 46 / 45 / 46.5)
   x.item_keys = x.rows > 32 ? 320 : p->format == HERMES_PAGE_FP4 ? 1024 : 512;
   // Without cuts a launch takes rounds of items; with cuts its steps are shared out, whatever
   // the lengths, at the price of a second launch and of the parts (5 to 10 us).  So there
   // are none where the longest items' rounds are short, in keys, and cuts would save
-  // little of them even if all were as long.  A workgroup of eight waves fits a CU; of the
-  // few-row kernel also two of four, which hide the start of one item behind another's
-  // keys where there are items enough (256 sequences of 1000 tokens, 4 KV heads: 38 us, 50
-  // with eight).  A step is 32 keys for each wave, or a tile for each key group.
+  // little of them even if all were as long.  Without and with, us, 28 + 4 heads of 128 in FP4:
+  // one row of 28 sequences of 2000 tokens 15.8 / 20.0, of 4 of 2500 15.9 / 13.1; 64 rows of 10
+  // of 300 20.5 / 31.6, of 4 of 1500 54.6 / 33.6.  (Near its bounds the rule is not always
+  // right: one bf16 row on 2000 tokens 26.3 / 15.8 goes without, one row of 256 sequences of 1900
+  // 51.3 / 72.8 with.)
+  // A workgroup of eight waves fits a CU; of the few-row kernel also two of four, which hide
+  // the start of one item behind another's keys where there are items enough (256 sequences of
+  // 1000 tokens 33.6 us, 45.6 with eight waves; 128 of 1000 18.7 and 24.6).  A step is 32 keys for
+  // each wave, or a tile for each key group.
   const bool few = x.rows <= 32;
   const int64_t tiles = over(P, x.rows), all = (int64_t)b->n_seqs * p->n_kv_heads * tiles;
   const int64_t items = all < 1 << 24 ? all : 1 << 24;   // (as good as more: cut, and products below 2^63)
