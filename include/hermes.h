@@ -541,8 +541,9 @@ int hermes_page_append(const hermes_page_pool *pool, const hermes_page_batch *ba
                        int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                        const int32_t *rope, void *q_out, void *stream);
 
-/* Bytes of workspace that hermes_page_attend needs for calls of `batch` (its
- * device pointers are not looked at; 0 if none, or on bad arguments). */
+/* Bytes of workspace that hermes_page_attend needs for calls of `batch` (of its
+ * device pointers only whether row_start is NULL matters; 0 if none, or on bad
+ * arguments). */
 size_t hermes_page_workspace_bytes(const hermes_page_pool *pool, const hermes_page_batch *batch);
 
 /*
