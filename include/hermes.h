@@ -449,9 +449,12 @@ enum {
                                   stored, and read as zeros                           */
   HERMES_PAGE_BAD_LENGTH = 2,  /* a length below 0 or beyond the sequence's table: the
                                   sequence counts as empty                            */
-  HERMES_PAGE_BAD_ROWS = 4     /* row starts that fall, or leave 0 .. n_rows: clamped (a
+  HERMES_PAGE_BAD_ROWS = 4,    /* row starts that fall, or leave 0 .. n_rows: clamped (a
                                   row that two sequences then hold gets the results of
                                   one of them)                                        */
+  HERMES_PAGE_BAD_PARENT = 8,  /* a parent beyond the sequence's beams: the beam is empty */
+  HERMES_PAGE_NO_ROOM = 16     /* a reorder found no page for a beam's rows in its room, or
+                                  no entry in its table: the entry is -1, or absent    */
 };
 
 /*
@@ -585,6 +588,151 @@ int hermes_page_read(const hermes_page_pool *pool, const hermes_page_batch *batc
  */
 int hermes_page_pack(hermes_ctx *ctx, int32_t layer, const hermes_page_pool *pool, const int32_t *tables,
                      int32_t max_pages, int32_t *kv_len, void *stream);
+
+/*
+ * Reorder the pages of beams: after a choice of continuations (hermes_beam_select) beam j
+ * of sequence s goes on from beam parent[s][j], in every layer.  A group is the beams of
+ * one sequence in one layer; groups stand layer by layer (group g is sequence g % n_seqs).
+ * The new table of a beam with n tokens (its parent's length) holds
+ *   - the parent's full pages, shared;
+ *   - where n is no multiple of page_rows, the parent's last page if nothing else of the
+ *     group holds it: it lies in the group's room, is no full page of a new beam and
+ *     the last page of no earlier one.  Else a page of the room, into which the rows
+ *     the last page holds are copied (up to a multiple of four rows; its other bytes stay);
+ *   - pages of the room for `grow` tokens more;
+ *   - and -1 behind them.
+ * Pages of the room are given out in ascending order, beam by beam, and are those that no
+ * new table of the group holds: what no beam goes on with is free again.  So appends
+ * of up to `grow` tokens a beam touch pages that no other beam reads, and pages
+ * outside the room (a memory or prompt that several groups share) are never written.
+ *  n_groups     a multiple of n_seqs (0 is allowed: the call does nothing), n_groups x n_beams
+ *               2^22 at most.
+ *  n_beams      beams of a sequence, 1 to 64.
+ *  max_pages    entries of a table; max_pages x page_rows is 2^31 - 257 at most.
+ *  grow         tokens that every beam gets room for, 0 to 2^20.
+ *  parent       device int32 [n_seqs][n_beams]; -1: the new beam is empty (length 0, no pages).
+ *  room         device int32 [n_groups][2]: the first page of the group's room and its number
+ *               of pages, 65536 at most.  Rooms of different groups hold no page in common.  A room
+ *               that does not lie in the pool counts as empty (HERMES_PAGE_BAD_ID).
+ *  tables, kv_len          device int32 [n_groups][n_beams][max_pages] and [n_groups][n_beams].
+ *  tables_out, kv_len_out  the new ones, apart from the old.
+ * The old tables must not be used again once rows have been appended by the new ones.
+ * As for the calls above, nothing that device memory holds leads out of bounds.
+ * Errors: EINVAL, ENOTSUP, EHIP.
+ */
+typedef struct {
+  int32_t n_groups;
+  int32_t n_seqs;
+  int32_t n_beams;
+  int32_t max_pages;
+  int32_t grow;
+  const int32_t *parent;
+  const int32_t *room;
+  const int32_t *tables;
+  const int32_t *kv_len;
+  int32_t *tables_out;
+  int32_t *kv_len_out;
+} hermes_page_beams;
+int hermes_page_reorder(const hermes_page_pool *pool, const hermes_page_beams *beams, void *stream);
+
+/*
+ * Beam search's choice: the n_keep best continuations of every sequence.  Token t of beam b has
+ * the value
+ *     (score[s][b] - ln sum_u exp(logits[s][b][u])) + logits[s][b][t]
+ * in 64 bits (the logarithm itself to about 1e-8: beams are compared through it), a beam
+ * that is done the one token pad_token, of value score[s][b].  Chosen are the greatest
+ * values, a tie going to the lower beam and then to the lower token, and come in that order.  A
+ * token of logit -infinity is never chosen, nor is any of a beam whose score is not finite, or
+ * one of whose logits is NaN or +infinity.  Where fewer than n_keep remain, parent and token are
+ * -1, the score -infinity.
+ *  n_seqs       sequences (0 is allowed: the call does nothing).
+ *  n_beams      1 to 64; n_seqs x n_beams is 2^15 at most, and n_beams x n_vocab 2^30.
+ *  n_keep       1 to 64 (n_beams for a search that carries ended beams along as done, twice
+ *               that for one that collects them apart).
+ *  logits_type  HERMES_BF16 or HERMES_FP32.
+ *  end_token    the token that ends a sequence, or -1.
+ *  pad_token    what a done beam goes on with.
+ */
+enum { HERMES_BF16 = 0, HERMES_FP32 = 1 };
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_beams;
+  int32_t n_vocab;
+  int32_t n_keep;
+  int32_t logits_type;
+  int32_t end_token;
+  int32_t pad_token;
+} hermes_beam_config;
+
+/* Bytes of workspace that hermes_beam_select needs (0 on a bad config, or if it has nothing to do). */
+size_t hermes_beam_workspace_bytes(const hermes_beam_config *cfg);
+
+/*
+ *  logits       device bf16 or fp32, n_seqs x n_beams rows of n_vocab, `stride` elements apart
+ *               (any stride from n_vocab to 2^32: the rows of a padded vocabulary, or odd ones).
+ *  score        device fp32 [n_seqs][n_beams].
+ *  done         device int32 [n_seqs][n_beams], other than 0: the beam has ended (its logits are
+ *               not read).  NULL: none has.
+ *  score_out    device fp32 [n_seqs][n_keep], the values rounded once.
+ *  parent_out, token_out   device int32 [n_seqs][n_keep].
+ *  done_out     device int32 [n_seqs][n_keep] or NULL: 1 where the parent is done or the token is
+ *               end_token.
+ *  workspace    device memory of hermes_beam_workspace_bytes, 16-byte aligned; free again when the
+ *               call's work is done.
+ * No output may be part of an input.  Runs on `stream` of the current device, allocates nothing, keeps
+ * nothing, and never synchronises; calls at once need a workspace each.
+ * Errors: EINVAL, ECAPACITY (workspace too small), EHIP.
+ */
+int hermes_beam_select(const hermes_beam_config *cfg, const void *logits, int64_t stride, const float *score,
+                       const int32_t *done, float *score_out, int32_t *parent_out, int32_t *token_out,
+                       int32_t *done_out, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * A weight in 4 bits, for products with few rows: FP4 as in the pages, with a power-of-two scale
+ * for every 32 inputs of an output.
+ * Layout: output n, input k lie in tile (n / 16, k / 128).  With N = ceil(n_out / 16) and K =
+ * ceil(n_in / 128) the codes are [N][K][64][16] bytes: lane 16 x (k % 128 / 32) + n % 16 of its tile,
+ * byte k % 32 / 2, the even input in the low half.  Behind them lie the scales, [N][ceil(K / 4)]
+ * [64][4] bytes: of the same lane, byte K-tile % 4.  Outputs and inputs past the weight's are zeros.
+ *  n_out        outputs, 1 to 2^24.
+ *  n_in         inputs, 1 to 2^20.
+ *  data         device memory of hermes_weight_bytes, 16-byte aligned.
+ */
+typedef struct {
+  int32_t n_out;
+  int32_t n_in;
+  void *data;
+} hermes_weight;
+
+/* Bytes of a weight's memory (0 on bad sizes; data is not looked at). */
+size_t hermes_weight_bytes(const hermes_weight *w);
+
+/*
+ * Store a weight: dense is device bf16, n_out rows of n_in, `stride` elements apart (any stride
+ * from n_in to 2^32).
+ * Errors: EINVAL, EHIP.
+ */
+int hermes_weight_pack(const hermes_weight *w, const void *dense, int64_t stride, void *stream);
+
+/*
+ * out[r][n] = sum_k x[r][k] W[n][k] + bias[n] + add[r][n], summed in fp32 and rounded once.
+ *  x            device bf16, n_rows rows of n_in, x_stride elements apart (a multiple of 8,
+ *               2^32 at most; 16-byte aligned).
+ *  n_rows       0 (the call does nothing) to 2^20.  Meant for few: the weight is read once for every 64.
+ *  bias         device bf16 [n_out], or NULL.
+ *  add          device bf16 [n_rows][n_out], or NULL; may be out, where that is bf16.
+ *  out          device [n_rows][n_out] of out_type HERMES_BF16 or HERMES_FP32, 16-byte aligned, apart
+ *               from x.
+ *  workspace    device memory of hermes_weight_workspace_bytes, 16-byte aligned (may be NULL if that is
+ *               0); free again when the call's work is done.
+ * Runs on `stream` of the current device, allocates nothing, keeps nothing, and never synchronises; calls
+ * at once need a workspace each.
+ * Errors: EINVAL, ECAPACITY (workspace too small), EHIP.
+ */
+size_t hermes_weight_workspace_bytes(const hermes_weight *w, int32_t n_rows);
+int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_stride, int32_t n_rows,
+                          const void *bias, const void *add, void *out, int32_t out_type, void *workspace,
+                          size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,232 @@
+// Host side of what stands around a generated token: products with weights in 4 bits, the
+// choice over beams, and the reordering of their pages.  Argument checks, sizes and launches;
+// nothing here keeps state or allocates.
+#include <cstdint>
+#include <cstring>
+
+#include "tokens_internal.h"
+
+using namespace hermes;
+
+namespace {
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+constexpr int64_t kMaxStride = INT64_C(1) << 32;   // (an end of rows is counted in 64 bits)
+int64_t over(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+bool overlap(const void *p, int64_t n, const void *q, int64_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p != nullptr && q != nullptr && a < b + (uintptr_t)m && b < a + (uintptr_t)n;
+}
+
+int check_weight(const hermes_weight *w) {
+  if (w == nullptr || w->n_out < 1 || w->n_out > 1 << 24 || w->n_in < 1 || w->n_in > 1 << 20) return HERMES_EINVAL;
+  return HERMES_OK;
+}
+
+WeightView view_of(const hermes_weight *w) {
+  WeightView v;
+  v.n_out = w->n_out;
+  v.n_in = w->n_in;
+  v.tiles_out = (int32_t)over(w->n_out, 16);
+  v.tiles_in = (int32_t)over(w->n_in, 128);
+  v.quads = (int32_t)over(v.tiles_in, 4);
+  v.codes = static_cast<uint8_t *>(w->data);
+  v.scales = v.codes + (int64_t)v.tiles_out * v.tiles_in * 1024;
+  return v;
+}
+
+int64_t bytes_of(const WeightView &v) {
+  return (int64_t)v.tiles_out * v.tiles_in * 1024 + (int64_t)v.tiles_out * v.quads * 256;
+}
+
+WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
+  WeightPlan p;
+  p.row_tiles = n_rows <= 16 ? 1 : n_rows <= 32 ? 2 : 4;
+  p.tiles = 1;
+  p.split = 8;
+  while (p.split > v.quads) p.split /= 2;
+  return p;
+}
+
+int check_beams(const hermes_beam_config *c) {
+  if (c == nullptr || c->n_seqs < 0 || c->n_beams < 1 || c->n_beams > kMaxBeams || c->n_vocab < 1) return HERMES_EINVAL;
+  if (c->n_keep < 1 || c->n_keep > kMaxKeep) return HERMES_EINVAL;
+  if ((int64_t)c->n_seqs * c->n_beams > 1 << 15 || (int64_t)c->n_beams * c->n_vocab > 1 << 30) return HERMES_EINVAL;
+  if (c->logits_type != HERMES_BF16 && c->logits_type != HERMES_FP32) return HERMES_EINVAL;
+  if (c->end_token < -1 || c->end_token >= c->n_vocab) return HERMES_EINVAL;
+  if (c->pad_token < 0 || c->pad_token >= c->n_vocab) return HERMES_EINVAL;
+  return HERMES_OK;
+}
+
+// Rows' waves take so many chunks that some thousands of waves are left.
+void cut_of(const hermes_beam_config *c, BeamArgs *a) {
+  const int64_t rows = (int64_t)c->n_seqs * c->n_beams;
+  a->chunks = (int32_t)over(c->n_vocab, kBeamChunk);
+  const int64_t per = rows * a->chunks / 8192;
+  a->per = (int32_t)(per < 1 ? 1 : per > 16 ? 16 : per);
+  a->parts = (int32_t)over(a->chunks, a->per);
+}
+
+struct BeamRoom { int64_t sum, peak, top, all; };
+BeamRoom beam_room(const BeamArgs &a, int64_t rows) {
+  BeamRoom r;
+  r.sum = 0;
+  r.peak = 8 * rows * a.parts;
+  r.top = r.peak + 4 * rows * a.parts;
+  r.all = over(r.top + 4 * rows * a.chunks, 16) * 16;
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hermes_weight_bytes(const hermes_weight *w) {
+  return check_weight(w) == HERMES_OK ? (size_t)bytes_of(view_of(w)) : 0;
+}
+
+int hermes_weight_pack(const hermes_weight *w, const void *dense, int64_t stride, void *stream) {
+  const int rc = check_weight(w);
+  if (rc != HERMES_OK) return rc;
+  if (w->data == nullptr || !aligned(w->data, 16)) return HERMES_EINVAL;
+  if (dense == nullptr || !aligned(dense, 2) || stride < w->n_in || stride > kMaxStride) return HERMES_EINVAL;
+  WeightPackArgs a;
+  a.w = view_of(w);
+  a.dense = static_cast<const uint16_t *>(dense);
+  a.stride = stride;
+  if (overlap(w->data, bytes_of(a.w), dense, 2 * ((w->n_out - 1) * stride + w->n_in))) return HERMES_EINVAL;
+  return launch_weight_pack(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
+}
+
+size_t hermes_weight_workspace_bytes(const hermes_weight *w, int32_t n_rows) {
+  (void)w;
+  (void)n_rows;
+  return 0;
+}
+
+int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_stride, int32_t n_rows,
+                          const void *bias, const void *add, void *out, int32_t out_type, void *workspace,
+                          size_t ws_bytes, void *stream) {
+  const int rc = check_weight(w);
+  if (rc != HERMES_OK) return rc;
+  if (n_rows < 0 || n_rows > 1 << 20) return HERMES_EINVAL;
+  if (out_type != HERMES_BF16 && out_type != HERMES_FP32) return HERMES_EINVAL;
+  if (w->data == nullptr || !aligned(w->data, 16)) return HERMES_EINVAL;
+  if (n_rows == 0) return HERMES_OK;
+  if (x == nullptr || !aligned(x, 16) || x_stride < w->n_in || x_stride > kMaxStride || x_stride % 8 != 0) return HERMES_EINVAL;
+  if (out == nullptr || !aligned(out, 16) || !aligned(bias, 2) || !aligned(add, 2)) return HERMES_EINVAL;
+  WeightProductArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.w = view_of(w);
+  const int64_t n = (int64_t)n_rows * w->n_out, size = out_type == HERMES_FP32 ? 4 : 2;
+  if (overlap(out, n * size, x, 2 * ((n_rows - 1) * x_stride + w->n_in))) return HERMES_EINVAL;
+  if (overlap(out, n * size, bias, 2 * (int64_t)w->n_out) || overlap(out, n * size, w->data, bytes_of(a.w))) return HERMES_EINVAL;
+  if (overlap(out, n * size, add, 2 * n) && (add != out || out_type != HERMES_BF16)) return HERMES_EINVAL;
+  (void)workspace;
+  (void)ws_bytes;
+  a.x = static_cast<const uint16_t *>(x);
+  a.bias = static_cast<const uint16_t *>(bias);
+  a.add = static_cast<const uint16_t *>(add);
+  a.out = out;
+  a.x_stride = x_stride;
+  a.n_rows = n_rows;
+  a.fp32 = out_type == HERMES_FP32;
+  a.plan = plan_of(a.w, n_rows);
+  return launch_weight_product(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
+}
+
+size_t hermes_beam_workspace_bytes(const hermes_beam_config *cfg) {
+  if (check_beams(cfg) != HERMES_OK) return 0;
+  BeamArgs a;
+  cut_of(cfg, &a);
+  return (size_t)beam_room(a, (int64_t)cfg->n_seqs * cfg->n_beams).all;
+}
+
+int hermes_beam_select(const hermes_beam_config *cfg, const void *logits, int64_t stride, const float *score,
+                       const int32_t *done, float *score_out, int32_t *parent_out, int32_t *token_out,
+                       int32_t *done_out, void *workspace, size_t ws_bytes, void *stream) {
+  const int rc = check_beams(cfg);
+  if (rc != HERMES_OK) return rc;
+  if (cfg->n_seqs == 0) return HERMES_OK;
+  const int64_t rows = (int64_t)cfg->n_seqs * cfg->n_beams, size = cfg->logits_type == HERMES_FP32 ? 4 : 2;
+  if (logits == nullptr || !aligned(logits, size) || stride < cfg->n_vocab || stride > kMaxStride) return HERMES_EINVAL;
+  if (score == nullptr || !aligned(score, 4) || !aligned(done, 4)) return HERMES_EINVAL;
+  const int64_t in_bytes = size * ((rows - 1) * stride + cfg->n_vocab), out_bytes = 4 * (int64_t)cfg->n_seqs * cfg->n_keep;
+  const void *outs[] = {score_out, parent_out, token_out, done_out};
+  for (int i = 0; i < 4; ++i) {
+    if (outs[i] == nullptr && i < 3) return HERMES_EINVAL;
+    if (!aligned(outs[i], 4) || overlap(outs[i], out_bytes, logits, in_bytes)) return HERMES_EINVAL;
+    if (overlap(outs[i], out_bytes, score, 4 * rows) || overlap(outs[i], out_bytes, done, 4 * rows)) return HERMES_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], out_bytes, outs[j], out_bytes)) return HERMES_EINVAL;
+  }
+  BeamArgs a;
+  std::memset(&a, 0, sizeof(a));
+  cut_of(cfg, &a);
+  const BeamRoom room = beam_room(a, rows);
+  if (workspace == nullptr || !aligned(workspace, 16)) return HERMES_EINVAL;
+  if (ws_bytes < (size_t)room.all) return HERMES_ECAPACITY;
+  char *ws = static_cast<char *>(workspace);
+  a.sum = reinterpret_cast<double *>(ws + room.sum);
+  a.peak = reinterpret_cast<float *>(ws + room.peak);
+  a.top = reinterpret_cast<float *>(ws + room.top);
+  a.logits = logits;
+  a.score = score;
+  a.done = done;
+  a.score_out = score_out;
+  a.parent_out = parent_out;
+  a.token_out = token_out;
+  a.done_out = done_out;
+  a.stride = stride;
+  a.n_seqs = cfg->n_seqs;
+  a.n_beams = cfg->n_beams;
+  a.n_vocab = cfg->n_vocab;
+  a.n_keep = cfg->n_keep;
+  a.end_token = cfg->end_token;
+  a.pad_token = cfg->pad_token;
+  return launch_beam_select(a, cfg->logits_type == HERMES_FP32, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? HERMES_OK : HERMES_EHIP;
+}
+
+int hermes_page_reorder(const hermes_page_pool *pool, const hermes_page_beams *beams, void *stream) {
+  const int rc = check_page_memory(pool);
+  if (rc != HERMES_OK) return rc;
+  const hermes_page_beams *b = beams;
+  if (b == nullptr || b->n_groups < 0 || b->n_beams < 1 || b->n_beams > kMaxBeams) return HERMES_EINVAL;
+  if (b->grow < 0 || b->grow > 1 << 20) return HERMES_EINVAL;
+  if (b->n_groups == 0) return HERMES_OK;
+  if (b->n_seqs < 1 || b->n_groups % b->n_seqs != 0 || (int64_t)b->n_groups * b->n_beams > 1 << 22) return HERMES_EINVAL;
+  if (b->max_pages < 1 || (int64_t)b->max_pages * pool->page_rows > INT32_MAX - 256) return HERMES_EINVAL;
+  const void *all[] = {b->parent, b->room, b->tables, b->kv_len, b->tables_out, b->kv_len_out};
+  const int64_t rows = (int64_t)b->n_groups * b->n_beams;
+  const int64_t bytes[] = {4 * (int64_t)b->n_seqs * b->n_beams, 8 * (int64_t)b->n_groups, 4 * rows * b->max_pages,
+                           4 * rows, 4 * rows * b->max_pages, 4 * rows};
+  for (int i = 0; i < 6; ++i) {
+    if (all[i] == nullptr || !aligned(all[i], 4)) return HERMES_EINVAL;
+    for (int j = 0; i >= 4 && j < i; ++j)
+      if (overlap(all[i], bytes[i], all[j], bytes[j])) return HERMES_EINVAL;
+  }
+  PageReorderArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.pool = page_pool_of(pool);
+  a.parent = b->parent;
+  a.room = b->room;
+  a.tables = b->tables;
+  a.kv_len = b->kv_len;
+  a.tables_out = b->tables_out;
+  a.kv_len_out = b->kv_len_out;
+  a.n_groups = b->n_groups;
+  a.n_seqs = b->n_seqs;
+  a.n_beams = b->n_beams;
+  a.max_pages = b->max_pages;
+  a.grow = b->grow;
+  const bool fp4 = pool->format == HERMES_PAGE_FP4;
+  a.row_bytes = fp4 ? pool->head_dim / 2 : 2 * pool->head_dim;
+  a.scale_bytes = fp4 ? pool->head_dim / 32 : 0;
+  const int64_t shares = kStreamSlots / b->n_groups;
+  a.shares = (int32_t)(shares < 1 ? 1 : shares > 8 ? 8 : shares);
+  return launch_page_reorder(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
+}
+
+}  // extern "C"

@@ -29,7 +29,8 @@ KERNEL_NAMES = ("append", "attention", "colsum", "select", "gather", "query", "s
 REINDEX_NONE, REINDEX_EAGER, REINDEX_LAZY = 0, 1, 2
 SCORE_CHUNK, SCORE_GUIDANCE = 0, 1
 PAGE_BF16, PAGE_FP4 = 0, 1
-PAGE_BAD_ID, PAGE_BAD_LENGTH, PAGE_BAD_ROWS = 1, 2, 4
+PAGE_BAD_ID, PAGE_BAD_LENGTH, PAGE_BAD_ROWS, PAGE_BAD_PARENT, PAGE_NO_ROOM = 1, 2, 4, 8, 16
+BF16, FP32 = 0, 1
 
 EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_append_chunk_at", "hermes_guidance_score", "hermes_compress",
@@ -39,7 +40,9 @@ EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_select_topk", "hermes_profile_enable", "hermes_profile_read",
             "hermes_check_enable", "hermes_kv_init_static",
             "hermes_page_bytes", "hermes_page_workspace_bytes", "hermes_page_append",
-            "hermes_page_attend", "hermes_page_read", "hermes_page_pack")
+            "hermes_page_attend", "hermes_page_read", "hermes_page_pack", "hermes_page_reorder",
+            "hermes_beam_workspace_bytes", "hermes_beam_select", "hermes_weight_bytes",
+            "hermes_weight_pack", "hermes_weight_workspace_bytes", "hermes_weight_product")
 STATIC_WORKSPACE_BYTES = 128 << 20
 
 
@@ -82,6 +85,23 @@ class PageBatchStruct(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
                 ("max_len", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("row_start", ctypes.c_void_p),
                 ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p)]
+
+
+class PageBeamsStruct(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("n_beams", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("grow", ctypes.c_int32), ("parent", ctypes.c_void_p),
+                ("room", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("tables_out", ctypes.c_void_p), ("kv_len_out", ctypes.c_void_p)]
+
+
+class BeamConfig(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_beams", ctypes.c_int32), ("n_vocab", ctypes.c_int32),
+                ("n_keep", ctypes.c_int32), ("logits_type", ctypes.c_int32), ("end_token", ctypes.c_int32),
+                ("pad_token", ctypes.c_int32)]
+
+
+class WeightStruct(ctypes.Structure):
+    _fields_ = [("n_out", ctypes.c_int32), ("n_in", ctypes.c_int32), ("data", ctypes.c_void_p)]
 
 
 _vp, _i32, _i64, _dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
@@ -142,6 +162,21 @@ lib.hermes_page_read.restype = ctypes.c_int
 lib.hermes_page_read.argtypes = [_pool_p, _batch_p, _vp, _vp, _vp]
 lib.hermes_page_pack.restype = ctypes.c_int
 lib.hermes_page_pack.argtypes = [_vp, _i32, _pool_p, _vp, _i32, _vp, _vp]
+lib.hermes_page_reorder.restype = ctypes.c_int
+lib.hermes_page_reorder.argtypes = [_pool_p, ctypes.POINTER(PageBeamsStruct), _vp]
+_beam_p, _weight_p = ctypes.POINTER(BeamConfig), ctypes.POINTER(WeightStruct)
+lib.hermes_beam_workspace_bytes.restype = ctypes.c_size_t
+lib.hermes_beam_workspace_bytes.argtypes = [_beam_p]
+lib.hermes_beam_select.restype = ctypes.c_int
+lib.hermes_beam_select.argtypes = [_beam_p, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+lib.hermes_weight_bytes.restype = ctypes.c_size_t
+lib.hermes_weight_bytes.argtypes = [_weight_p]
+lib.hermes_weight_pack.restype = ctypes.c_int
+lib.hermes_weight_pack.argtypes = [_weight_p, _vp, _i64, _vp]
+lib.hermes_weight_workspace_bytes.restype = ctypes.c_size_t
+lib.hermes_weight_workspace_bytes.argtypes = [_weight_p, _i32]
+lib.hermes_weight_product.restype = ctypes.c_int
+lib.hermes_weight_product.argtypes = [_weight_p, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp, ctypes.c_size_t, _vp]
 
 
 class HermesError(RuntimeError):
@@ -179,6 +214,15 @@ def _need(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> None:
                          f"{getattr(t, 'dtype', None)} {tuple(getattr(t, 'shape', ()))}")
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: must be a contiguous device tensor")
+
+
+def _on(index: int, fn, name: str, *args) -> None:
+    """fn(*args, stream) with device `index` current, on its current stream."""
+    if _raw_stream is not None and _device() == index:
+        check(fn(*args, _raw_stream(index)), name)
+    else:
+        with torch.cuda.device(index):
+            check(fn(*args, _stream()), name)
 
 
 def budget_from_weights(weights: Sequence[float], total: int) -> list:
@@ -524,11 +568,7 @@ class KVPages:
     # (a token's calls are a few microseconds on the device: their checks are kept short)
     def _run(self, fn, name: str, *args) -> None:
         """fn(*args, stream) with the pool's device current."""
-        if _raw_stream is not None and _device() == self._index:
-            check(fn(*args, _raw_stream(self._index)), name)
-        else:
-            with torch.cuda.device(self.device):
-                check(fn(*args, _stream()), name)
+        _on(self._index, fn, name, *args)
 
     def _on_device(self, t: torch.Tensor, name: str) -> None:
         if t.get_device() != self._index:
@@ -614,10 +654,131 @@ class KVPages:
         self._run(lib.hermes_page_read, "hermes_page_read", self._ref, batch._ref, k.data_ptr(), v.data_ptr())
         return k, v
 
+    def reorder(self, tables: torch.Tensor, kv_len: torch.Tensor, parent: torch.Tensor, room: torch.Tensor, grow: int = 1,
+                tables_out: Optional[torch.Tensor] = None, kv_len_out: Optional[torch.Tensor] = None):
+        """The (tables, kv_len) that beams go on with after a choice: beam j of sequence s continues
+        beam parent[s][j] (int32 [n_seqs][n_beams]; -1: none), in every layer.  tables int32
+        [n_seqs][n_beams][max_pages], or with layers before them; kv_len likewise without pages;
+        room int32 [.., n_seqs][2], first page and number of pages of the beams' own pages.
+        Full pages are shared, a partly filled one that is not a beam's own is copied, and there
+        is room for `grow` tokens more (hermes_page_reorder)."""
+        if not isinstance(tables, torch.Tensor) or tables.dim() < 3:
+            raise ValueError("tables: expected [n_seqs][n_beams][max_pages], or with layers before them")
+        shape = tables.shape
+        n_seqs, n_beams, max_pages = shape[-3:]
+        self._fits(tables, torch.int32, shape, "tables")
+        self._fits(kv_len, torch.int32, shape[:-1], "kv_len")
+        self._fits(parent, torch.int32, (n_seqs, n_beams), "parent")
+        self._fits(room, torch.int32, shape[:-2] + (2,), "room")
+        if tables_out is None:
+            tables_out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        else:
+            self._fits(tables_out, torch.int32, shape, "tables_out")
+        if kv_len_out is None:
+            kv_len_out = torch.empty(shape[:-1], dtype=torch.int32, device=self.device)
+        else:
+            self._fits(kv_len_out, torch.int32, shape[:-1], "kv_len_out")
+        s = PageBeamsStruct(math.prod(shape[:-2]), n_seqs, n_beams, max_pages, grow, parent.data_ptr(), room.data_ptr(),
+                            tables.data_ptr(), kv_len.data_ptr(), tables_out.data_ptr(), kv_len_out.data_ptr())
+        self._run(lib.hermes_page_reorder, "hermes_page_reorder", self._ref, ctypes.byref(s))
+        return tables_out, kv_len_out
+
     def faults(self) -> int:
         bits = int(self._status.item())
         self._status.zero_()
         return bits
+
+
+def beam_select(logits: torch.Tensor, score: torch.Tensor, keep: int, done: Optional[torch.Tensor] = None,
+                end_token: int = -1, pad_token: int = 0):
+    """The `keep` best continuations of every sequence (hermes_beam_select): logits bf16 or fp32
+    [n_seqs][n_beams][n_vocab], whose rows may lie apart; score fp32 [n_seqs][n_beams]; done
+    int32 likewise, other than 0 where a beam has ended.  Returns score fp32, parent, token and
+    done int32, all [n_seqs][keep], the best first; parent and token are -1 where there are fewer."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits: expected torch.bfloat16 or torch.float32 [n_seqs][n_beams][n_vocab]")
+    n_seqs, n_beams, n_vocab = logits.shape
+    if not logits.is_cuda:
+        raise ValueError("logits: must be a device tensor")
+    ss, stride, es = logits.stride()
+    if n_beams == 1 or logits.numel() == 0:
+        stride = ss
+    if logits.numel() == 0 or n_seqs * n_beams == 1:
+        stride = max(n_vocab, 1)
+    elif n_seqs > 1 and ss != n_beams * stride:
+        raise ValueError("logits: rows must lie evenly apart")
+    if es != 1 and n_vocab > 1:
+        raise ValueError("logits: a row must be contiguous")
+    for t, dtype, name in ((score, torch.float32, "score"), (done, torch.int32, "done")):
+        if t is None and name == "done":
+            continue
+        _need(t, dtype, (n_seqs, n_beams), name)
+        if t.device != logits.device:
+            raise ValueError(f"{name}: a tensor on {t.device}, the logits are on {logits.device}")
+    cfg = BeamConfig(n_seqs, n_beams, n_vocab, keep, FP32 if logits.dtype is torch.float32 else BF16, end_token, pad_token)
+    nbytes = lib.hermes_beam_workspace_bytes(ctypes.byref(cfg))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+    out = torch.empty((4, n_seqs, max(keep, 0)), dtype=torch.int32, device=logits.device)
+    best, parent, token, ended = out.unbind(0)
+    best = best.view(torch.float32)
+    _on(logits.get_device(), lib.hermes_beam_select, "hermes_beam_select", ctypes.byref(cfg), logits.data_ptr(), stride,
+        score.data_ptr(), _ptr(done), best.data_ptr(), parent.data_ptr(), token.data_ptr(), ended.data_ptr(),
+        ws.data_ptr(), nbytes)
+    return best, parent, token, ended
+
+
+class PackedWeight:
+    """A weight in 4 bits (hermes_weight), made of `dense`, bf16 [n_out][n_in], which is not kept.
+
+    Calls run on the current stream of its device; the weight is laid out when it is made, on the
+    stream that is current then."""
+
+    def __init__(self, dense: torch.Tensor):
+        if not isinstance(dense, torch.Tensor) or dense.dim() != 2 or dense.dtype is not torch.bfloat16:
+            raise ValueError("dense: expected torch.bfloat16 [n_out][n_in]")
+        if not dense.is_cuda or (dense.stride(1) != 1 and dense.shape[1] > 1):
+            raise ValueError("dense: must be a device tensor with contiguous rows")
+        self.n_out, self.n_in = dense.shape
+        self.device, self._index = dense.device, dense.get_device()
+        w = WeightStruct(self.n_out, self.n_in, None)
+        nbytes = lib.hermes_weight_bytes(ctypes.byref(w))
+        if nbytes == 0:
+            raise HermesError(EINVAL, "hermes_weight_bytes")
+        self.data = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        w.data = self.data.data_ptr()
+        self._weight, self._ref = w, ctypes.byref(w)
+        _on(self._index, lib.hermes_weight_pack, "hermes_weight_pack", self._ref, dense.data_ptr(),
+            dense.stride(0) if self.n_out > 1 else self.n_in)
+
+    def product(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """x [n_rows][n_in] (bf16, rows may lie apart) times the weight's transpose, plus bias [n_out]
+        and add [n_rows][n_out] (bf16): [n_rows][n_out] of bf16 or fp32 (`dtype`, or `out`'s).
+        out may be add."""
+        if not isinstance(x, torch.Tensor) or x.dtype is not torch.bfloat16 or x.dim() != 2 or x.shape[1] != self.n_in:
+            raise ValueError(f"x: expected torch.bfloat16 [n_rows][{self.n_in}], got {getattr(x, 'dtype', None)} "
+                             f"{tuple(getattr(x, 'shape', ()))}")
+        n = x.shape[0]
+        shape = (n, self.n_out)
+        if out is None:
+            if dtype is not torch.bfloat16 and dtype is not torch.float32:
+                raise ValueError("dtype: torch.bfloat16 or torch.float32")
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+        elif not isinstance(out, torch.Tensor) or out.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("out: expected torch.bfloat16 or torch.float32")
+        for t, want, type_, name in ((bias, (self.n_out,), torch.bfloat16, "bias"), (add, shape, torch.bfloat16, "add"),
+                                     (out, shape, out.dtype, "out")):
+            if t is not None and (t.dtype is not type_ or t.shape != want or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected contiguous {type_} {want}, got {t.dtype} {tuple(t.shape)}")
+        for t in (x, bias, add, out):
+            if t is not None and t.get_device() != self._index:
+                raise ValueError(f"product: a tensor on {t.device}, the weight is on {self.device}")
+        if n and x.stride(1) != 1 and self.n_in > 1:
+            raise ValueError("x: a row must be contiguous")
+        stride = x.stride(0) if n > 1 else -(-self.n_in // 8) * 8
+        _on(self._index, lib.hermes_weight_product, "hermes_weight_product", self._ref, x.data_ptr(), stride, n, _ptr(bias),
+            _ptr(add), out.data_ptr(), FP32 if out.dtype is torch.float32 else BF16, None, 0)
+        return out
 
 
 def default_sm_scale(head_dim: int) -> float:

@@ -1,0 +1,55 @@
+// What the kernels around a generated token use beyond hip_runtime.h, on the CPU.  MFMAs
+// leave their sums as they are.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+template <typename T>
+T any_lane(T x, int l) {
+  static_assert(sizeof(T) <= 8);
+  int64_t bits = 0;
+  std::memcpy(&bits, &x, sizeof(T));
+  bits = cpu::across(bits, [&](int64_t *v) { return v[l & 63]; });
+  T y;
+  std::memcpy(&y, &bits, sizeof(T));
+  return y;
+}
+inline float __shfl_xor(float x, int m) { return any_lane(x, cpu::lane() ^ m); }
+inline double __shfl_xor(double x, int m) { return any_lane(x, cpu::lane() ^ m); }
+inline int __shfl(int x, int l) { return any_lane(x, l); }
+inline double __shfl(double x, int l) { return any_lane(x, l); }
+inline uint32_t atomicOr(uint32_t *p, uint32_t bits) { return __atomic_fetch_or(p, bits, __ATOMIC_SEQ_CST); }
+inline int atomicAdd(int32_t *p, int n) { return __atomic_fetch_add(p, n, __ATOMIC_SEQ_CST); }
+inline unsigned long long atomicAdd(unsigned long long *p, unsigned long long n) {
+  return __atomic_fetch_add(p, n, __ATOMIC_SEQ_CST);
+}
+template <typename A, typename B, typename C>
+C same(A, B, C c, int, int, int) { return c; }
+
+#define __builtin_amdgcn_exp2f(x) std::exp2(x)
+#define __builtin_amdgcn_mfma_f32_16x16x32_bf16(...) same(__VA_ARGS__)
+
+#include <sys/mman.h>
+
+#include <cstdio>
+
+// `bytes` of memory that end where the next page begins, which cannot be touched, and begin
+// behind one that cannot (to the page).
+inline void *guarded(size_t bytes, size_t align) {
+  const size_t size = (bytes + 4095) / 4096 * 4096;
+  char *m = static_cast<char *>(mmap(nullptr, size + 8192, PROT_NONE, MAP_PRIVATE | MAP_ANONYMOUS, -1, 0)) + 4096;
+  if (size > 0 && mprotect(m, size, PROT_READ | PROT_WRITE) != 0) std::abort();
+  return m + (size - bytes) / align * align;
+}
+
+// An array of `n` from standard input.
+template <typename T>
+T *input(size_t n, size_t align = sizeof(T)) {
+  T *p = static_cast<T *>(guarded(n * sizeof(T), align));
+  if (std::fread(p, sizeof(T), n, stdin) != n) std::abort();
+  return p;
+}
+template <typename T>
+void output(const T *p, size_t n) {
+  if (std::fwrite(p, sizeof(T), n, stdout) != n) std::abort();
+}
