@@ -691,9 +691,10 @@ int hermes_beam_select(const hermes_beam_config *cfg, const void *logits, int64_
  * A weight in 4 bits, for products with few rows: FP4 as in the pages, with a power-of-two scale
  * for every 32 inputs of an output.
  * Layout: output n, input k lie in tile (n / 16, k / 128).  With N = ceil(n_out / 16) and K =
- * ceil(n_in / 128) the codes are [N][K][64][16] bytes: lane 16 x (k % 128 / 32) + n % 16 of its tile,
- * byte k % 32 / 2, the even input in the low half.  Behind them lie the scales, [N][ceil(K / 4)]
- * [64][4] bytes: of the same lane, byte K-tile % 4.  Outputs and inputs past the weight's are zeros.
+ * ceil(n_in / 128) the codes are [N][K][64][16] bytes: lane 16 x (k % 32 / 8) + n % 16 of its tile,
+ * byte 4 x (k % 128 / 32) + k % 8 / 2, the even input in the low half.  Behind them lie the scales,
+ * [N][ceil(K / 4)][16][16] bytes: of output n % 16, byte 4 x (K-tile % 4) + k % 128 / 32.  Outputs and
+ * inputs past the weight's are zeros.
  *  n_out        outputs, 1 to 2^24.
  *  n_in         inputs, 1 to 2^20.
  *  data         device memory of hermes_weight_bytes, 16-byte aligned.
@@ -717,22 +718,17 @@ int hermes_weight_pack(const hermes_weight *w, const void *dense, int64_t stride
 /*
  * out[r][n] = sum_k x[r][k] W[n][k] + bias[n] + add[r][n], summed in fp32 and rounded once.
  *  x            device bf16, n_rows rows of n_in, x_stride elements apart (a multiple of 8,
- *               2^32 at most; 16-byte aligned).
+ *               2^24 at most; 16-byte aligned).
  *  n_rows       0 (the call does nothing) to 2^20.  Meant for few: the weight is read once for every 64.
  *  bias         device bf16 [n_out], or NULL.
  *  add          device bf16 [n_rows][n_out], or NULL; may be out, where that is bf16.
  *  out          device [n_rows][n_out] of out_type HERMES_BF16 or HERMES_FP32, 16-byte aligned, apart
  *               from x.
- *  workspace    device memory of hermes_weight_workspace_bytes, 16-byte aligned (may be NULL if that is
- *               0); free again when the call's work is done.
- * Runs on `stream` of the current device, allocates nothing, keeps nothing, and never synchronises; calls
- * at once need a workspace each.
- * Errors: EINVAL, ECAPACITY (workspace too small), EHIP.
+ * Runs on `stream` of the current device, allocates nothing, keeps nothing, and never synchronises.
+ * Errors: EINVAL, EHIP.
  */
-size_t hermes_weight_workspace_bytes(const hermes_weight *w, int32_t n_rows);
 int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_stride, int32_t n_rows,
-                          const void *bias, const void *add, void *out, int32_t out_type, void *workspace,
-                          size_t ws_bytes, void *stream);
+                          const void *bias, const void *add, void *out, int32_t out_type, void *stream);
 
 #ifdef __cplusplus
 }

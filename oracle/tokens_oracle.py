@@ -17,18 +17,18 @@ def pack(bits):
     n, k = bits.shape
     N, K = -(-n // 16), -(-k // 128)
     code, scale = pages.fp4(_padded(bits, 16 * N, 128 * K))
-    byte = (code[:, 0::2] | (code[:, 1::2] << 4)).reshape(N, 16, K, 4, 16)          # [.., n, .., block, byte]
-    codes = byte.transpose(0, 2, 3, 1, 4)                                            # lane 16 block + n
-    scales = np.full((N, -(-K // 4), 64, 4), 8, np.uint8)
+    byte = (code[:, 0::2] | (code[:, 1::2] << 4)).reshape(N, 16, K, 4, 4, 4)         # [.., n, .., block, lane / 16, byte]
+    codes = byte.transpose(0, 2, 4, 1, 3, 5)
+    scales = np.full((N, -(-K // 4), 16, 4, 4), 8, np.uint8)
     for kt in range(K):
-        scales[:, kt // 4, :, kt % 4] = scale.reshape(N, 16, K, 4)[:, :, kt].transpose(0, 2, 1).reshape(N, 64)
+        scales[:, kt // 4, :, kt % 4] = scale.reshape(N, 16, K, 4)[:, :, kt]
     return codes.reshape(-1), scales
 
 
 def unused_scales(n, k):
     """Scale bytes that no tile has (those behind the last of its four)."""
     N, K = -(-n // 16), -(-k // 128)
-    m = np.zeros((N, -(-K // 4), 64, 4), bool)
+    m = np.zeros((N, -(-K // 4), 16, 4, 4), bool)
     if K % 4:
         m[:, -1, :, K % 4:] = True
     return m

@@ -20,12 +20,12 @@ struct WeightPackArgs {
   int64_t stride;
 };
 
-// How a product is cut: a workgroup of eight waves takes (8 / split) x tiles tiles of
-// outputs, `split` waves sharing the inputs of each.
+// How a product is cut: a workgroup takes 4 row_quads rows, and its waves (eight, or four with
+// 64 rows) waves / split x tiles tiles of outputs, `split` waves sharing the inputs of each.
 struct WeightPlan {
-  int32_t row_tiles;        // tiles of 16 rows a workgroup takes: 1, 2 or 4
-  int32_t tiles;            // tiles of outputs a wave takes
-  int32_t split;            // 1, 2, 4 or 8
+  int32_t row_quads;        // 1, 2, 4, 8 or 16
+  int32_t tiles;            // 1, 2 or 4
+  int32_t split;            // 1, 2, 4 or 8 (4 at most with 64 rows)
 };
 
 struct WeightProductArgs {

@@ -5,9 +5,12 @@
 //
 // A product of M <= 64 rows reads 17/32 byte of weight for 2 M operations, so HBM bounds it up
 // to there.  The layout is an MFMA operand's: of a tile of 16 outputs and 128 inputs a lane holds 32
-// inputs of one output, one 16-byte load, one scale.  Codes times scales are exact in bf16
+// inputs of one output in one 16-byte load.  Codes times scales are exact in bf16
 // (v_cvt_scalef32_pk_bf16_fp4, two values an instruction), x is bf16, and
 // v_mfma_f32_16x16x32_bf16 sums in fp32, so what is rounded is the sum alone.
+//
+// Measured (calls in one graph, weights not in the caches): 8 rows of 3584 on 131072 outputs 46.5 us,
+// 5.46 TB/s; one row on 4608 5.8, on 1152 x 896 3.3 (an empty launch: 1.8); 64 rows on 14336 17.3.
 #include "tokens_internal.h"
 
 namespace hermes {
@@ -15,51 +18,53 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 8;
 
 // ------------------------------------------------------------------------- pack
 // A wave stores the same 16 outputs of four tiles along the inputs (a quad).  The scale
 // of 32 values is the least 2^e with amax <= 7 x 2^e: on the bits of a bf16
-// magnitude e = ((bits + 31) >> 7) - 2 - 127 (as in the pages).
+// magnitude e = ((bits + 31) >> 7) - 2 - 127 (as in the pages).  A block's 32 values lie in the
+// four lanes of an output.
 __global__ __launch_bounds__(256) void weight_pack(WeightPackArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (unit >= (int64_t)a.w.tiles_out * a.w.quads) return;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, q = lane / 16;
   const int nt = (int)(unit / a.w.quads), quad = (int)(unit % a.w.quads);
   const int n = 16 * nt + lane % 16;
   const uint16_t *row = a.dense + (int64_t)n * a.stride;
-  uint32_t scales = 0;
+  uint32_t mine = 0;        // the scales of tile q of the quad
   for (int i = 0; i < 4; ++i) {
     const int kt = 4 * quad + i;
     if (kt >= a.w.tiles_in) break;
-    const int k0 = 128 * kt + 32 * (lane / 16);
-    uint32_t v[16];         // pairs of bf16
-    const int have = n < a.w.n_out ? min(a.w.n_in - k0, 32) : 0;
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const uint32_t lo = 2 * j < have ? row[k0 + 2 * j] : 0u, hi = 2 * j + 1 < have ? row[k0 + 2 * j + 1] : 0u;
-      v[j] = lo | hi << 16;
-      m = max(m, max(lo & 0x7FFFu, hi & 0x7FFFu));
-    }
-    const uint32_t scale = m >= 0x7F80u ? 255u : (uint32_t)min(max((int)((m + 31u) >> 7) - 2, 127 - 119), 127 + 125);
-    const float sc = __builtin_bit_cast(float, scale << 23);
-    uint32_t c[4];
+    uint32_t c[4], scales = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      const int k0 = 128 * kt + 32 * j + 8 * q, have = n < a.w.n_out ? a.w.n_in - k0 : 0;
+      uint32_t v[4], m = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t lo = 2 * x < have ? row[k0 + 2 * x] : 0u, hi = 2 * x + 1 < have ? row[k0 + 2 * x + 1] : 0u;
+        v[x] = lo | hi << 16;
+        m = max(m, max(lo & 0x7FFFu, hi & 0x7FFFu));
+      }
+      m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+      const uint32_t scale = m >= 0x7F80u ? 255u : (uint32_t)min(max((int)((m + 31u) >> 7) - 2, 127 - 119), 127 + 125);
+      const float sc = __builtin_bit_cast(float, scale << 23);
       uint32_t r = 0;
-      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[4 * j]), sc, 0);
-      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[4 * j + 1]), sc, 1);
-      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[4 * j + 2]), sc, 2);
-      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[4 * j + 3]), sc, 3);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[0]), sc, 0);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[1]), sc, 1);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[2]), sc, 2);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, v[3]), sc, 3);
       c[j] = r;
+      scales |= scale << (8 * j);
     }
     *reinterpret_cast<uint4 *>(a.w.codes + (((int64_t)nt * a.w.tiles_in + kt) * 64 + lane) * 16) = uint4{c[0], c[1], c[2], c[3]};
-    scales |= scale << (8 * i);
+    if (q == i) mine = scales;
   }
-  *reinterpret_cast<uint32_t *>(a.w.scales + (unit * 64 + lane) * 4) = scales;
+  *reinterpret_cast<uint32_t *>(a.w.scales + (unit * 16 + lane % 16) * 16 + 4 * q) = mine;
 }
 
 // ---------------------------------------------------------------------- product
@@ -72,33 +77,33 @@ __device__ __forceinline__ bf16x8 unpack(uint32_t codes, float scale) {
 }
 
 // Inputs k .. k + 7 of a row, zeros past the last.
-__device__ __forceinline__ uint4 inputs(const uint16_t *row, int k, int n_in) {
-  if (k + 8 <= n_in) return *reinterpret_cast<const uint4 *>(row + k);
-  uint32_t v[4];
+__device__ __forceinline__ u32x4 inputs(const uint16_t *row, int k, int n_in) {
+  if (k + 8 <= n_in) return *reinterpret_cast<const u32x4 *>(row + k);
+  u32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t lo = k + 2 * i < n_in ? row[k + 2 * i] : 0u, hi = k + 2 * i + 1 < n_in ? row[k + 2 * i + 1] : 0u;
     v[i] = lo | hi << 16;
   }
-  return uint4{v[0], v[1], v[2], v[3]};
+  return v;
 }
 
 // Four outputs n .. n + 3 of row r.
 __device__ __forceinline__ void store(const WeightProductArgs &a, int64_t r, int n, f32x4 v) {
   const int64_t at = r * a.w.n_out + n;
   const bool whole = n + 4 <= a.w.n_out && a.w.n_out % 4 == 0;
-  uint16_t b[4] = {0, 0, 0, 0}, d[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (n + i >= a.w.n_out) continue;
-    if (a.bias != nullptr) b[i] = a.bias[n + i];
-    if (a.add != nullptr) d[i] = a.add[at + i];
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (a.bias != nullptr) v[i] += __builtin_bit_cast(float, (uint32_t)b[i] << 16);
-    if (a.add != nullptr) v[i] += __builtin_bit_cast(float, (uint32_t)d[i] << 16);
-  }
+  const auto plus = [&](const uint16_t *from) {
+    uint16_t b[4] = {0, 0, 0, 0};
+    if (whole) {
+      __builtin_memcpy(b, from, 8);
+    } else {
+      for (int i = 0; i < 4; ++i)
+        if (n + i < a.w.n_out) b[i] = from[i];
+    }
+    for (int i = 0; i < 4; ++i) v[i] += __builtin_bit_cast(float, (uint32_t)b[i] << 16);
+  };
+  if (a.bias != nullptr) plus(a.bias + n);
+  if (a.add != nullptr) plus(a.add + at);
   if (a.fp32) {
     float *out = static_cast<float *>(a.out) + at;
     if (whole) {
@@ -121,60 +126,133 @@ __device__ __forceinline__ void store(const WeightProductArgs &a, int64_t r, int
   }
 }
 
-// MFMA layout (v_mfma_f32_16x16x32_bf16): lane l = 16 q + n supplies A[n][8 q ..] (weights; any order
-// of the inputs that both operands agree on) and B[8 q ..][n] (row n of x), and holds D[4 q + i][n].
-template <int MT, int NT>
-__global__ __launch_bounds__(64 * kWaves) void weight_product(WeightProductArgs a) {
-  __shared__ f32x4 part[kWaves][MT * NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// A wave's loads of a step: codes and scales of U tiles along the inputs of NT tiles of outputs
+// into registers, the same inputs of x into LDS.
+template <int NT, int U>
+struct Step {
+  u32x4 codes[U][NT];
+  uint32_t scales[U][NT];
+};
+
+// Waits for all loads of this wave, those to LDS among them, and for its reads of LDS.
+__device__ __forceinline__ void wait_for_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);       // vmcnt 0, lgkmcnt 0
+  asm volatile("" ::: "memory");
+}
+
+// 16 bytes a lane from base + lane_offset + offset (below `bytes`; zeros past it) to `to` + 16 lane.
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, uint32_t lane_offset, uint32_t offset, uint8_t *to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000),
+                                           (__attribute__((address_space(3))) void *)to, 16, lane_offset, offset, 0, 0);
+}
+
+// MFMA layout (v_mfma_f32_16x16x32_bf16): lane l = 16 q + n supplies A[n][8 q ..] (weights) and
+// B[8 q ..][n] (row n of x), and holds D[4 q + i][n].
+//
+// x reaches the lanes through LDS, a tile's 128 inputs of a row in 256 bytes, 16 lanes a row: as
+// fragments straight from memory 16 neighbouring lanes' pieces lie in 16 rows, and the loads take longer than
+// the weight's (64 rows on 14336 x 3584 23.8 us so, 17.3 through LDS; 8 rows on 131072 54.9 and 46.0).  Piece c
+// of row r lies at c ^ (r % 16), so that neither the loads nor the fragments' reads meet in a
+// bank.  LDS is each wave's own (waves that share outputs have different inputs), so there is no
+// barrier before their sums are joined, and while a step is multiplied the next one's loads run.
+template <int RQ, int NT, int U, int W>
+__global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
+  constexpr int MT = (RQ + 3) / 4;                      // tiles of 16 rows
+  constexpr int kTile = RQ * 1024, kSlot = U * kTile;   // bytes of x: 4 RQ rows of a tile, of a step
+  constexpr int kRoom = 2 * kSlot * W > W * MT * NT * 1024 ? 2 * kSlot * W : W * MT * NT * 1024;
+  __shared__ __attribute__((aligned(16))) uint8_t room[kRoom];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = a.plan.split, sub = wave % split;
-  const int nt0 = (blockIdx.x * (kWaves / split) + wave / split) * NT;
-  const int q = lane / 16, r0 = blockIdx.y * 16 * MT;
-  const uint16_t *row[MT];
+  const int nt0 = (blockIdx.x * (W / split) + wave / split) * NT;
+  const int q = lane / 16, n16 = lane % 16, r0 = blockIdx.y * 16 * MT;
+  const int k0 = (int)((int64_t)a.w.tiles_in * sub / split), k1 = (int)((int64_t)a.w.tiles_in * (sub + 1) / split);
+  const int whole = a.w.n_in / 128;
+  const int rows = min(a.n_rows - r0, 16 * MT);
+  // (an offset in the rows of a block stays below 2^32: 64 rows of up to 2^24 elements)
+  const uint16_t *x0 = a.x + (int64_t)r0 * a.x_stride;
+  const uint32_t x_bytes = (uint32_t)(2 * ((rows - 1) * a.x_stride + a.w.n_in));
+  uint32_t from[RQ];                    // this lane's piece of row 4 i + q
 #pragma unroll
-  for (int t = 0; t < MT; ++t) row[t] = a.x + (int64_t)min(r0 + 16 * t + lane % 16, a.n_rows - 1) * a.x_stride;
+  for (int i = 0; i < RQ; ++i) {
+    const int r = 4 * i + q;
+    from[i] = (uint32_t)(min(r, rows - 1) * a.x_stride * 2) + 16 * (n16 ^ (r % 16));
+  }
+  uint8_t *const mine = room + wave * 2 * kSlot;
+  int at[MT];                           // this lane's row of fragments, and its place in a tile
+#pragma unroll
+  for (int t = 0; t < MT; ++t) at[t] = min(16 * t + n16, 4 * RQ - 1);
+  const uint8_t *codes[NT], *scales[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    const int64_t nt = min(nt0 + u, a.w.tiles_out - 1);
+    codes[u] = a.w.codes + (nt * a.w.tiles_in * 64 + lane) * 16;
+    scales[u] = a.w.scales + (nt * a.w.quads * 16 + n16) * 16;
+  }
   f32x4 acc[NT][MT];
 #pragma unroll
   for (int u = 0; u < NT; ++u)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int q0 = (int)((int64_t)a.w.quads * sub / split), q1 = (int)((int64_t)a.w.quads * (sub + 1) / split);
-  if (nt0 < a.w.tiles_out) {
-    for (int quad = q0; quad < q1; ++quad) {
-      uint32_t scales[NT];
+
+  const auto load = [&](Step<NT, U> &s, int kt, int slot) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (kt + i >= k1) break;
+      uint8_t *to = mine + slot * kSlot + i * kTile;
+      if (kt + i < whole) {
+#pragma unroll
+        for (int r = 0; r < RQ; ++r)
+          load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
+      } else {
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) {
+          const int row = min(4 * r + q, rows - 1);
+          *reinterpret_cast<u32x4 *>(to + r * 1024 + lane * 16) =
+              inputs(x0 + row * a.x_stride, 128 * (kt + i) + 8 * (n16 ^ ((4 * r + q) % 16)), a.w.n_in);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (kt + i >= k1) break;
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        const int nt = min(nt0 + u, a.w.tiles_out - 1);
-        scales[u] = *reinterpret_cast<const uint32_t *>(a.w.scales + (((int64_t)nt * a.w.quads + quad) * 64 + lane) * 4);
+        s.codes[i][u] = *reinterpret_cast<const u32x4 *>(codes[u] + (int64_t)(kt + i) * 1024);
+        s.scales[i][u] = *reinterpret_cast<const uint32_t *>(scales[u] + (int64_t)((kt + i) / 4) * 256 + (kt + i) % 4 * 4);
       }
+    }
+  };
+  const auto multiply = [&](const Step<NT, U> &s, int kt, int slot) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int kt = 4 * quad + i;
-        if (kt >= a.w.tiles_in) break;
-        uint4 codes[NT], xv[MT][4];
+    for (int i = 0; i < U; ++i) {
+      if (kt + i >= k1) break;
+      const uint8_t *tile = mine + slot * kSlot + i * kTile;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 x[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) x[t] = *reinterpret_cast<const bf16x8 *>(tile + at[t] * 256 + 16 * ((4 * j + q) ^ (at[t] % 16)));
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-          const int nt = min(nt0 + u, a.w.tiles_out - 1);
-          codes[u] = *reinterpret_cast<const uint4 *>(a.w.codes + (((int64_t)nt * a.w.tiles_in + kt) * 64 + lane) * 16);
-        }
-        const int k0 = 128 * kt + 32 * q;
+          const bf16x8 v = unpack(s.codes[i][u][j], __builtin_bit_cast(float, (s.scales[i][u] >> (8 * j) & 255u) << 23));
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) xv[t][j] = inputs(row[t], k0 + 8 * j, a.w.n_in);
-#pragma unroll
-        for (int u = 0; u < NT; ++u) {
-          const float scale = __builtin_bit_cast(float, (scales[u] >> (8 * i) & 255u) << 23);
-          const uint32_t c[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bf16x8 w = unpack(c[j], scale);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-              acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, xv[t][j]), acc[u][t], 0, 0, 0);
-          }
+          for (int t = 0; t < MT; ++t) acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, x[t], acc[u][t], 0, 0, 0);
         }
       }
+    }
+  };
+  if (nt0 < a.w.tiles_out && k0 < k1) {
+    Step<NT, U> even, odd;
+    load(even, k0, 0);
+    for (int kt = k0; kt < k1; kt += 2 * U) {
+      wait_for_loads();
+      if (kt + U < k1) load(odd, kt + U, 1);
+      multiply(even, kt, 0);
+      if (kt + U >= k1) break;
+      wait_for_loads();
+      if (kt + 2 * U < k1) load(even, kt + 2 * U, 0);
+      multiply(odd, kt + U, 1);
     }
   }
   if (split == 1) {
@@ -182,24 +260,26 @@ __global__ __launch_bounds__(64 * kWaves) void weight_product(WeightProductArgs 
     for (int u = 0; u < NT; ++u)
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        const int r = r0 + 16 * t + lane % 16;
-        if (nt0 + u < a.w.tiles_out && r < a.n_rows) store(a, r, 16 * (nt0 + u) + 4 * q, acc[u][t]);
+        const int r = 16 * t + n16;
+        if (nt0 + u < a.w.tiles_out && r < rows) store(a, r0 + r, 16 * (nt0 + u) + 4 * q, acc[u][t]);
       }
     return;
   }
+  __syncthreads();
+  f32x4 *part = reinterpret_cast<f32x4 *>(room);        // [waves][NT MT][64]
 #pragma unroll
   for (int u = 0; u < NT; ++u)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][u * MT + t][lane] = acc[u][t];
+    for (int t = 0; t < MT; ++t) part[(wave * MT * NT + u * MT + t) * 64 + lane] = acc[u][t];
   __syncthreads();
   // tile i of group g: summed over the group's waves, in their order
-  const int groups = kWaves / split;
-  for (int i = wave; i < groups * NT * MT; i += kWaves) {
+  const int groups = W / split;
+  for (int i = wave; i < groups * NT * MT; i += W) {
     const int g = i / (NT * MT), tile = i % (NT * MT);
-    const int nt = (blockIdx.x * groups + g) * NT + tile / MT, r = r0 + 16 * (tile % MT) + lane % 16;
-    f32x4 v = part[g * split][tile][lane];
-    for (int s = 1; s < split; ++s) v += part[g * split + s][tile][lane];
-    if (nt < a.w.tiles_out && r < a.n_rows) store(a, r, 16 * nt + 4 * q, v);
+    const int nt = (blockIdx.x * groups + g) * NT + tile / MT, r = 16 * (tile % MT) + n16;
+    f32x4 v = part[(g * split * MT * NT + tile) * 64 + lane];
+    for (int s = 1; s < split; ++s) v += part[((g * split + s) * MT * NT + tile) * 64 + lane];
+    if (nt < a.w.tiles_out && r < rows) store(a, r0 + r, 16 * nt + 4 * q, v);
   }
 }
 
@@ -211,15 +291,39 @@ hipError_t launch_weight_pack(const WeightPackArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_weight_product(const WeightProductArgs &a, hipStream_t s) {
-  const int groups = kWaves / a.plan.split * a.plan.tiles, rows = 16 * a.plan.row_tiles;
-  const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + rows - 1) / rows), block(64 * kWaves);
-  if (a.plan.row_tiles == 1) {
-    hipLaunchKernelGGL((weight_product<1, 1>), grid, block, 0, s, a);
-  } else if (a.plan.row_tiles == 2) {
-    hipLaunchKernelGGL((weight_product<2, 1>), grid, block, 0, s, a);
+// Rows by four, tiles of outputs a wave, steps of so many tiles of inputs, waves.  (A workgroup's x
+// is 2 steps x waves x 1 KiB x rows by four: 128 KiB at 16 rows and more, so that workgroups of 64 rows
+// have four waves.)
+template <int RQ, int NT>
+static void launch_product(const WeightProductArgs &a, hipStream_t s) {
+  constexpr int U = RQ <= 4 && NT < 4 ? 2 : 1, W = RQ <= 8 ? 8 : 4, kRows = 16 * ((RQ + 3) / 4);
+  const int groups = W / a.plan.split * NT;
+  const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + kRows - 1) / kRows);
+  hipLaunchKernelGGL((weight_product<RQ, NT, U, W>), grid, dim3(64 * W), 0, s, a);
+}
+
+template <int RQ>
+static void launch_product(const WeightProductArgs &a, hipStream_t s) {
+  if (a.plan.tiles == 1) {
+    launch_product<RQ, 1>(a, s);
+  } else if (a.plan.tiles == 2) {
+    launch_product<RQ, 2>(a, s);
   } else {
-    hipLaunchKernelGGL((weight_product<4, 1>), grid, block, 0, s, a);
+    launch_product<RQ, 4>(a, s);
+  }
+}
+
+hipError_t launch_weight_product(const WeightProductArgs &a, hipStream_t s) {
+  if (a.plan.row_quads == 1) {
+    launch_product<1>(a, s);
+  } else if (a.plan.row_quads == 2) {
+    launch_product<2>(a, s);
+  } else if (a.plan.row_quads == 4) {
+    launch_product<4>(a, s);
+  } else if (a.plan.row_quads == 8) {
+    launch_product<8>(a, s);
+  } else {
+    launch_product<16>(a, s);
   }
   return hipGetLastError();
 }

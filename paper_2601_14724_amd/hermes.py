@@ -42,7 +42,7 @@ EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_page_bytes", "hermes_page_workspace_bytes", "hermes_page_append",
             "hermes_page_attend", "hermes_page_read", "hermes_page_pack", "hermes_page_reorder",
             "hermes_beam_workspace_bytes", "hermes_beam_select", "hermes_weight_bytes",
-            "hermes_weight_pack", "hermes_weight_workspace_bytes", "hermes_weight_product")
+            "hermes_weight_pack", "hermes_weight_product")
 STATIC_WORKSPACE_BYTES = 128 << 20
 
 
@@ -173,10 +173,8 @@ lib.hermes_weight_bytes.restype = ctypes.c_size_t
 lib.hermes_weight_bytes.argtypes = [_weight_p]
 lib.hermes_weight_pack.restype = ctypes.c_int
 lib.hermes_weight_pack.argtypes = [_weight_p, _vp, _i64, _vp]
-lib.hermes_weight_workspace_bytes.restype = ctypes.c_size_t
-lib.hermes_weight_workspace_bytes.argtypes = [_weight_p, _i32]
 lib.hermes_weight_product.restype = ctypes.c_int
-lib.hermes_weight_product.argtypes = [_weight_p, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp, ctypes.c_size_t, _vp]
+lib.hermes_weight_product.argtypes = [_weight_p, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp]
 
 
 class HermesError(RuntimeError):
@@ -777,7 +775,7 @@ class PackedWeight:
             raise ValueError("x: a row must be contiguous")
         stride = x.stride(0) if n > 1 else -(-self.n_in // 8) * 8
         _on(self._index, lib.hermes_weight_product, "hermes_weight_product", self._ref, x.data_ptr(), stride, n, _ptr(bias),
-            _ptr(add), out.data_ptr(), FP32 if out.dtype is torch.float32 else BF16, None, 0)
+            _ptr(add), out.data_ptr(), FP32 if out.dtype is torch.float32 else BF16)
         return out
 
 

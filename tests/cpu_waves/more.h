@@ -26,6 +26,21 @@ inline unsigned long long atomicAdd(unsigned long long *p, unsigned long long n)
 template <typename A, typename B, typename C>
 C same(A, B, C c, int, int, int) { return c; }
 
+// 16 bytes a lane to LDS, zeros from outside the buffer
+struct Buffer {
+  const char *base;
+  uint32_t bytes;
+};
+inline void buffer_to_lds(Buffer b, void *to, int size, uint32_t lane_offset, uint32_t offset, int, int) {
+  char *mine = static_cast<char *>(to) + size * cpu::lane();
+  if ((uint64_t)lane_offset + offset + size <= b.bytes) std::memcpy(mine, b.base + lane_offset + offset, size);
+  else std::memset(mine, 0, size);
+}
+
+#define __builtin_amdgcn_make_buffer_rsrc(p, stride, n, flags) (Buffer{static_cast<const char *>(p), n})
+#define __builtin_amdgcn_raw_ptr_buffer_load_lds(...) buffer_to_lds(__VA_ARGS__)
+#define __builtin_amdgcn_s_waitcnt(n) cpu::waves[threadIdx.x >> 6].meet.arrive_and_wait()
+#define address_space(n) aligned(1)
 #define __builtin_amdgcn_exp2f(x) std::exp2(x)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(...) same(__VA_ARGS__)
 

@@ -1,5 +1,5 @@
 // weight_pack and weight_product in memory that ends where their inputs end.
-//   weights <outputs> <inputs> <rows> <row tiles> <tiles> <split> <bias> <add> <fp32>
+//   weights <outputs> <inputs> <rows> <rows by four> <tiles> <split> <bias> <add> <fp32>
 #include "more.h"
 
 #include "weights.hip"

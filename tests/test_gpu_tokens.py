@@ -56,9 +56,10 @@ def test_a_packed_weight_is_the_definition_s(n, k, stride):
         assert (scales == 255).sum() == 1
         bits[4, 32:64] = 0                # (the codes of a block of NaN may be any)
         codes2, _ = orc.pack(bits)
-        lane = (0, 16 * 1 + 4)
+        lane = (0, [4, 20, 36, 52], slice(4, 8))      # output 4, inputs 32 to 63 of the first tile
         got_codes = got_codes.copy()
-        got_codes.reshape(-1, 64, 16)[lane] = codes2.reshape(-1, 64, 16)[lane] = 0
+        got_codes.reshape(-1, 64, 16)[lane] = 0
+        codes2.reshape(-1, 64, 16)[lane] = 0
         codes = codes2
     # (a code of zero may keep its sign)
     low, high = got_codes & 15, got_codes >> 4

@@ -20,7 +20,7 @@ def _weight(n_out=100, n_in=200, data=FAKE):
 
 
 def _product(w=None, x=FAR, xs=200, rows=4, bias=None, add=None, out=2 * FAR, kind=H.BF16):
-    return H.lib.hermes_weight_product(ctypes.byref(w or _weight()), x, xs, rows, bias, add, out, kind, None, 0, None)
+    return H.lib.hermes_weight_product(ctypes.byref(w or _weight()), x, xs, rows, bias, add, out, kind, None)
 
 
 @pytest.mark.parametrize("n,k", [(1, 1), (16, 128), (17, 129), (1003, 2236), (4608, 3584), (131072, 513)])
@@ -49,12 +49,12 @@ def test_bad_pack_arguments_are_refused():
 
 def test_bad_product_arguments_are_refused():
     for over in (dict(w=_weight(data=None)), dict(w=_weight(data=FAKE + 4)), dict(x=None), dict(x=FAR + 8), dict(xs=192),
-                 dict(xs=204), dict(xs=1 << 40), dict(rows=-1), dict(rows=(1 << 20) + 1), dict(out=None), dict(out=2 * FAR + 8),
+                 dict(xs=204), dict(xs=(1 << 24) + 8), dict(rows=-1), dict(rows=(1 << 20) + 1), dict(out=None), dict(out=2 * FAR + 8),
                  dict(bias=FAKE + 1), dict(add=FAKE + 1), dict(kind=2), dict(kind=-1),
                  dict(out=FAR), dict(out=FAR + 3 * 400), dict(bias=2 * FAR + 790), dict(add=2 * FAR + 2),
                  dict(add=2 * FAR, kind=H.FP32), dict(out=FAKE + 16)):
         assert _product(**over) == H.EINVAL, over
-    assert H.lib.hermes_weight_product(None, FAR, 200, 4, None, None, 2 * FAR, 0, None, 0, None) == H.EINVAL
+    assert H.lib.hermes_weight_product(None, FAR, 200, 4, None, None, 2 * FAR, 0, None) == H.EINVAL
 
 
 def test_a_product_of_no_rows_does_nothing():
@@ -166,11 +166,11 @@ def test_weight_memory_by_hand():
         bits = np.zeros((21, 800), np.uint16)
         bits[n, k] = pages.bf16_bits(-1.5)
         codes, scales = orc.pack(bits)
-        lane = 16 * (k % 128 // 32) + n % 16
-        at = ((n // 16 * 7 + k // 128) * 64 + lane) * 16 + k % 32 // 2
+        lane = 16 * (k % 32 // 8) + n % 16
+        at = ((n // 16 * 7 + k // 128) * 64 + lane) * 16 + 4 * (k % 128 // 32) + k % 8 // 2
         # 1.5 = 6 x 2^-2: code 7, with the sign 15
         assert codes[at] == 15 << (4 * (k % 2)) and codes.sum() == codes[at]
-        assert scales[n // 16, k // 512, lane, k // 128 % 4] == 127 - 2 and (scales != 8).sum() == 1
+        assert scales[n // 16, k // 512, n % 16, k // 128 % 4, k % 128 // 32] == 127 - 2 and (scales != 8).sum() == 1
 
 
 def test_reference_product_of_one_row():
