@@ -15,6 +15,8 @@
 // Beams meet through ln sum exp, and what is chosen are whole numbers, so it is found to about 1e-8:
 // differences to a peak times log2 e in two fp32 steps (the second holds what log2 e as an
 // fp32 lacks), the hardware's exponential (1 ulp), eight of them added in fp32, all else in 64 bits.
+#include <type_traits>
+
 #include "tokens_internal.h"
 
 namespace hermes {
@@ -53,16 +55,44 @@ __device__ __forceinline__ void eight(const void *row, int i, int n, float *x) {
   for (int j = 0; j < 8; ++j) x[j] = i + j < n ? logit<FP32>(row, i + j) : -__builtin_inff();
 }
 
+// Moves between lanes: of 16 lanes, x ^ 1, x ^ 2, 7 - x, 15 - x; then the wave.
+template <int Ctrl>
+__device__ __forceinline__ int moved(int x) {
+  return __builtin_amdgcn_update_dpp(x, x, Ctrl, 0xF, 0xF, false);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRow15 = 0x142, kRow31 = 0x143;
+
+// The greatest of the wave's, in lane 63.
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x = fmaxf(x, __shfl_xor(x, m));
+  const auto with = [&](int y) { x = __builtin_fmaxf(x, __builtin_bit_cast(float, y)); };
+  with(moved<kXor1>(__builtin_bit_cast(int, x)));
+  with(moved<kXor2>(__builtin_bit_cast(int, x)));
+  with(moved<kHalfMirror>(__builtin_bit_cast(int, x)));
+  with(moved<kMirror>(__builtin_bit_cast(int, x)));
+  with(moved<kRow15>(__builtin_bit_cast(int, x)));
+  with(moved<kRow31>(__builtin_bit_cast(int, x)));
   return x;
 }
 
+template <int Ctrl, int Rows = 0xF>
+__device__ __forceinline__ double moved(double x) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, Ctrl, Rows, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), Ctrl, Rows, 0xF, false);
+  return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+// The sum of the wave's, in lane 63.
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-  return x;
+  x += moved<kXor1>(x);
+  x += moved<kXor2>(x);
+  x += moved<kHalfMirror>(x);
+  x += moved<kMirror>(x);
+  x += moved<kRow15, 0xA>(x);
+  return x + moved<kRow31, 0xC>(x);
+}
+
+__device__ __forceinline__ float last_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
 template <bool FP32>
@@ -79,30 +109,44 @@ __global__ __launch_bounds__(kRowThreads) void beam_rows(BeamArgs a) {
   const int c1 = min((part + 1) * a.per, a.chunks);
   float peak = -__builtin_inff();
   double sum = 0.0;
-  for (int c = part * a.per; c < c1; ++c) {
-    float x[8];
-    eight<FP32>(row, c * kBeamChunk + 8 * lane, a.n_vocab, x);
-    float m = x[0];
+  // P chunks at once: their loads and their maxima's moves are independent
+  const auto take = [&](int c, auto number) {
+    constexpr int P = decltype(number)::value;
+    float x[P][8], m[P], all;
 #pragma unroll
-    for (int j = 1; j < 8; ++j) m = fmaxf(m, x[j]);
-    m = wave_max(m);
-    if (lane == 0) a.top[(int64_t)r * a.chunks + c] = m;
-    if (m > peak) {
-      sum = peak == -__builtin_inff() ? 0.0 : sum * exp((double)peak - (double)m);
-      peak = m;
+    for (int i = 0; i < P; ++i) eight<FP32>(row, (c + i) * kBeamChunk + 8 * lane, a.n_vocab, x[i]);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      m[i] = x[i][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) m[i] = __builtin_fmaxf(m[i], x[i][j]);
+      m[i] = wave_max(m[i]);
+      if (lane == 63) a.top[(int64_t)r * a.chunks + c + i] = m[i];
+      all = i == 0 ? m[0] : __builtin_fmaxf(all, m[i]);
+    }
+    all = last_lane(all);
+    if (all > peak) {
+      sum = peak == -__builtin_inff() ? 0.0 : sum * exp((double)peak - (double)all);
+      peak = all;
     }
     // (all -infinity so far: against zero, they add nothing)
     const float base = peak == -__builtin_inff() ? 0.0f : peak;
-    float e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float d = x[j] - base;
-      e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2eHigh, d * kLog2eLow));
+    for (int i = 0; i < P; ++i) {
+      float e[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = x[i][j] - base;
+        e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2eHigh, d * kLog2eLow));
+      }
+      sum += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
     }
-    sum += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
-  }
+  };
+  int c = part * a.per;
+  for (; c + 4 <= c1; c += 4) take(c, std::integral_constant<int, 4>{});
+  for (; c < c1; ++c) take(c, std::integral_constant<int, 1>{});
   sum = wave_sum(sum);
-  if (lane == 0) {
+  if (lane == 63) {
     a.sum[(int64_t)r * a.parts + part] = sum;
     a.peak[(int64_t)r * a.parts + part] = peak;
   }
@@ -113,13 +157,15 @@ __global__ __launch_bounds__(kRowThreads) void beam_rows(BeamArgs a) {
 // those of value -infinity are none.
 __device__ __forceinline__ bool before(double v, int i, double w, int j) { return v > w || (v == w && i < j); }
 
-constexpr int kList = 2048;
+constexpr int kList = 2048, kPickWaves = kPickThreads / 64;
+static_assert(kPickThreads == 64 * 16, "64 groups of 16 threads");
 
 struct PickShared {
   double offset[kMaxBeams];         // score - ln sum exp; a done beam: its score; -infinity: offers nothing
   int32_t done[kMaxBeams];
-  double best_value[64];
-  int32_t best_index[64];
+  int32_t beam[kMaxKeep], token[kMaxKeep];   // the chosen chunks: beam and first token
+  double best_value[64], edge_value;
+  int32_t best_index[64], edge_index;
   double value[kList];
   int32_t index[kList];
   int32_t count;
@@ -128,107 +174,118 @@ struct PickShared {
   int32_t out_index[kMaxKeep];
 };
 
+struct Candidate {
+  double v;
+  int i;
+};
+template <int Ctrl>
+__device__ __forceinline__ Candidate first_of(const Candidate &x) {
+  const Candidate y{moved<Ctrl>(x.v), moved<Ctrl>(x.i)};
+  return before(y.v, y.i, x.v, x.i) ? y : x;
+}
+// The sum over 16 lanes.
+__device__ __forceinline__ int row_sum(int x) {
+  x += moved<kXor1>(x);
+  x += moved<kXor2>(x);
+  x += moved<kHalfMirror>(x);
+  return x + moved<kMirror>(x);
+}
+
 // Orders as the value does (-0 and 0 alike).
 __device__ __forceinline__ unsigned long long key_of(double v) {
   const unsigned long long u = __builtin_bit_cast(unsigned long long, v + 0.0);
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// How many of `n` candidates item(i, &value, &index) satisfy `test`.
-template <typename Item, typename Test>
-__device__ __forceinline__ unsigned long long count_items(PickShared &s, int n, Item &&item, Test &&test) {
+// A set of candidates is a function that calls another with (value, index) of each of this
+// thread's; those of value -infinity do not count.
+
+// How many satisfy `test`.
+template <typename Each, typename Test>
+__device__ __forceinline__ unsigned long long count_of(PickShared &s, const Each &each, Test &&test) {
   __syncthreads();
   if (threadIdx.x == 0) s.counted = 0;
   __syncthreads();
   unsigned long long mine = 0;
-  for (int i = threadIdx.x; i < n; i += kPickThreads) {
-    double v;
-    int j;
-    item(i, &v, &j);
-    if (v > kNone && test(v, j)) ++mine;
-  }
+  each([&](double v, int i) { mine += v > kNone && test(v, i); });
   if (mine != 0) atomicAdd(&s.counted, mine);
   __syncthreads();
   return s.counted;
 }
 
-// The `keep` first of n candidates, in order, to s.out_value and s.out_index; how many there are.
+// The keep-th candidate, bit by bit.
+template <typename Each>
+__device__ Candidate find_edge(PickShared &s, int keep, const Each &each) {
+  unsigned long long k = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const unsigned long long next = k | 1ull << bit;
+    if (count_of(s, each, [&](double v, int) { return key_of(v) >= next; }) >= (unsigned long long)keep) k = next;
+  }
+  const unsigned long long more = count_of(s, each, [&](double v, int) { return key_of(v) > k; });
+  int last = 0;             // of the candidates that tie, the lowest indexes
+  for (int bit = 30; bit >= 0; --bit) {
+    const int next = last | 1 << bit;
+    if (more + count_of(s, each, [&](double v, int i) { return key_of(v) == k && i < next; }) < (unsigned long long)keep)
+      last = next;
+  }
+  return Candidate{__builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k), last};
+}
+
+// The `keep` first candidates, in order, to s.out_value and s.out_index; how many there are.
 //
 // The first of each of 64 groups of candidates: the keep-th of those is a bound that at least
-// `keep` candidates reach, and few more do (the keep-th of 64 groups' greatest).  Those are listed, and
-// each counts the ones before it.  Where more reach the bound than the list holds, the bound
-// is raised to the keep-th candidate itself, bit by bit.
-template <typename Item>
-__device__ __forceinline__ int pick(PickShared &s, int keep, int n, Item &&item) {
-  const int tid = threadIdx.x;
-  double bv = kNone;
-  int bi = INT32_MAX;
-  for (int i = tid; i < n; i += kPickThreads) {
-    double v;
-    int j;
-    item(i, &v, &j);
-    if (before(v, j, bv, bi)) bv = v, bi = j;
-  }
-#pragma unroll
-  for (int m = 1; m < 16; m *= 2) {
-    const double v = __shfl_xor(bv, m);
-    const int j = __shfl_xor(bi, m);
-    if (before(v, j, bv, bi)) bv = v, bi = j;
-  }
+// `keep` candidates reach, and few more do.  Those are listed, and 16 threads each count the ones
+// before it.  Where more reach the bound than the list holds, the bound is raised to the keep-th
+// candidate itself (whole rows of ties: some 100 us).
+template <typename Each>
+__device__ __forceinline__ int pick(PickShared &s, int keep, const Each &each) {
+  const int tid = threadIdx.x, group = tid / 16, slice = tid % 16;
+  Candidate best{kNone, INT32_MAX};
+  each([&](double v, int i) {
+    if (before(v, i, best.v, best.i)) best = Candidate{v, i};
+  });
+  best = first_of<kXor1>(best);
+  best = first_of<kXor2>(best);
+  best = first_of<kHalfMirror>(best);
+  best = first_of<kMirror>(best);
   if (tid == 0) s.count = 0;
-  if (tid % 16 == 0) s.best_value[tid / 16] = bv, s.best_index[tid / 16] = bi;
+  if (slice == 0) s.best_value[group] = best.v, s.best_index[group] = best.i;
   __syncthreads();
-  double edge = s.best_value[tid & 63];
-  int edge_index = s.best_index[tid & 63];
-  {
-    int rank = 0;
-    for (int j = 0; j < 64; ++j) {
-      const double v = s.best_value[j];
-      const int x = s.best_index[j];
-      // (empty groups are alike: they take their place in the line)
-      rank += before(v, x, edge, edge_index) || (v == edge && x == edge_index && j < (tid & 63));
-    }
-    const int src = __builtin_ctzll(__ballot(rank == keep - 1));
-    edge = __shfl(edge, src);
-    edge_index = __shfl(edge_index, src);
+  int rank = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int g = slice + 16 * j;
+    const double v = s.best_value[g];
+    const int x = s.best_index[g];
+    // (empty groups are alike: they take their place in the line)
+    rank += before(v, x, best.v, best.i) || (v == best.v && x == best.i && g < group);
   }
+  rank = row_sum(rank);
+  if (rank == keep - 1 && slice == 0) s.edge_value = best.v, s.edge_index = best.i;
+  __syncthreads();
+  Candidate edge{s.edge_value, s.edge_index};
   for (int round = 0;; ++round) {
-    for (int i = tid; i < n; i += kPickThreads) {
-      double v;
-      int j;
-      item(i, &v, &j);
-      if (v > kNone && !before(edge, edge_index, v, j)) {
+    each([&](double v, int i) {
+      if (v > kNone && !before(edge.v, edge.i, v, i)) {
         const int at = atomicAdd(&s.count, 1);
-        if (at < kList) s.value[at] = v, s.index[at] = j;
+        if (at < kList) s.value[at] = v, s.index[at] = i;
       }
-    }
+    });
     __syncthreads();
     if (s.count <= kList || round > 0) break;
-    unsigned long long k = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const unsigned long long next = k | 1ull << bit;
-      if (count_items(s, n, item, [&](double v, int) { return key_of(v) >= next; }) >= (unsigned long long)keep) k = next;
-    }
-    const unsigned long long more = count_items(s, n, item, [&](double v, int) { return key_of(v) > k; });
-    int last = 0;           // of the candidates that tie, the lowest indexes
-    for (int bit = 30; bit >= 0; --bit) {
-      const int next = last | 1 << bit;
-      if (more + count_items(s, n, item, [&](double v, int j) { return key_of(v) == k && j < next; }) < (unsigned long long)keep)
-        last = next;
-    }
-    edge = __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
-    edge_index = last;
+    edge = find_edge(s, keep, each);
     __syncthreads();
     if (tid == 0) s.count = 0;
     __syncthreads();
   }
   const int count = min(s.count, kList);
-  for (int c = tid; c < count; c += kPickThreads) {
-    const double v = s.value[c];
-    const int j = s.index[c];
-    int rank = 0;
-    for (int o = 0; o < count; ++o) rank += before(s.value[o], s.index[o], v, j);
-    if (rank < keep) s.out_value[rank] = v, s.out_index[rank] = j;
+  for (int c0 = 0; c0 < count; c0 += 64) {
+    const int c = min(c0 + group, count - 1);
+    const Candidate x{s.value[c], s.index[c]};
+    int first = 0;
+    for (int o = slice; o < count; o += 16) first += before(s.value[o], s.index[o], x.v, x.i);
+    first = row_sum(first);
+    if (slice == 0 && c0 + group < count && first < keep) s.out_value[first] = x.v, s.out_index[first] = x.i;
   }
   __syncthreads();
   return min(count, keep);
@@ -237,56 +294,70 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, int n, Item &&item)
 template <bool FP32>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   __shared__ PickShared s;
-  __shared__ int32_t chosen[kMaxKeep];
-  const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row0 = (int64_t)seq * a.n_beams;
-  for (int b = tid >> 6; b < a.n_beams; b += kPickThreads / 64) {
+  const float *top = a.top + row0 * a.chunks;
+  // a beam's chunks belong to `share` waves
+  int share = kPickWaves;
+  while (share > 1 && share * a.n_beams > kPickWaves) share /= 2;
+  const int first_chunk = wave % share * 64 + lane;
+  // (asked for now, so that it is near when the sums are done)
+  const float near = wave / share < a.n_beams && first_chunk < a.chunks ? top[wave / share * a.chunks + first_chunk] : 0.0f;
+  for (int b = wave; b < a.n_beams; b += kPickWaves) {
     const int64_t r = row0 + b;
     const double score = a.score[r];
     const int done = a.done != nullptr && a.done[r] != 0;
     double offset = score;
     if (!done) {
+      const double *sums = a.sum + r * a.parts;
+      const float *peaks = a.peak + r * a.parts;
       float peak = -__builtin_inff();
-      for (int p = lane; p < a.parts; p += 64) peak = fmaxf(peak, a.peak[r * a.parts + p]);
-      peak = wave_max(peak);
+      for (int p = lane; p < a.parts; p += 64) peak = __builtin_fmaxf(peak, peaks[p]);
+      peak = last_lane(wave_max(peak));
       double sum = 0.0;     // (a NaN or an infinity of the row makes it a NaN)
       for (int p = lane; p < a.parts; p += 64) {
-        const double x = a.sum[r * a.parts + p];
-        const float at = a.peak[r * a.parts + p];
+        const double x = sums[p];
+        const float at = peaks[p];
         sum += at == peak ? x : x * exp((double)at - (double)peak);
       }
-      sum = wave_sum(sum);
-      offset = score - ((double)peak + log(sum));
+      offset = score - ((double)peak + log(wave_sum(sum)));
     }
-    if (lane == 0) {
+    if (lane == 63) {
       s.offset[b] = __builtin_isfinite(offset) ? offset : kNone;
       s.done[b] = done;
     }
   }
+  asm volatile("" ::"v"(near));
   __syncthreads();
-  const int pad_chunk = a.pad_token / kBeamChunk;
-  const int n_chunks = pick(s, a.n_keep, a.n_beams * a.chunks, [&](int i, double *v, int *index) {
-    const int b = i / a.chunks, c = i - b * a.chunks;
-    const double offset = s.offset[b];
-    *index = i;
-    if (s.done[b]) {
-      *v = c == pad_chunk ? offset : kNone;
-    } else {
-      *v = offset == kNone ? kNone : offset + (double)a.top[row0 * a.chunks + i];
+  const int n_chunks = pick(s, a.n_keep, [&](auto &&take) {
+    for (int b = wave / share; b < a.n_beams; b += kPickWaves / share) {
+      const double offset = s.offset[b];
+      if (offset == kNone) continue;
+      if (s.done[b]) {
+        if (first_chunk == 0) take(offset, b * a.chunks + a.pad_token / kBeamChunk);
+        continue;
+      }
+      for (int c = first_chunk; c < a.chunks; c += 64 * share) take(offset + (double)top[b * a.chunks + c], b * a.chunks + c);
     }
   });
-  if (tid < n_chunks) chosen[tid] = s.out_index[tid];
+  if (tid < n_chunks) {
+    const int i = s.out_index[tid], b = i / a.chunks;
+    s.beam[tid] = b;
+    s.token[tid] = (i - b * a.chunks) * kBeamChunk;
+  }
   __syncthreads();
-  const int n = pick(s, a.n_keep, n_chunks * kBeamChunk, [&](int i, double *v, int *index) {
-    const int x = chosen[i / kBeamChunk], b = x / a.chunks;
-    const int t = (x - b * a.chunks) * kBeamChunk + i % kBeamChunk;
-    *index = b * a.n_vocab + t;
-    *v = kNone;
-    if (t >= a.n_vocab) return;
-    if (s.done[b]) {
-      if (t == a.pad_token) *v = s.offset[b];
-    } else {
-      *v = s.offset[b] + (double)logit<FP32>(row_of<FP32>(a, row0 + b), t);
+  const int n = pick(s, a.n_keep, [&](auto &&take) {
+    for (int k = wave; k < n_chunks; k += kPickWaves) {
+      const int b = s.beam[k], t = s.token[k] + 8 * lane;
+      const double offset = s.offset[b];
+      if (s.done[b]) {
+        if (lane == 0) take(offset, b * a.n_vocab + a.pad_token);
+        continue;
+      }
+      float x[8];
+      eight<FP32>(row_of<FP32>(a, row0 + b), t, a.n_vocab, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) take(offset + (double)x[j], b * a.n_vocab + t + j);
     }
   });
   if (tid < a.n_keep) {

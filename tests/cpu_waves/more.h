@@ -26,6 +26,21 @@ inline unsigned long long atomicAdd(unsigned long long *p, unsigned long long n)
 template <typename A, typename B, typename C>
 C same(A, B, C c, int, int, int) { return c; }
 
+struct int2 { int x, y; };
+// The moves within 16 lanes that hip_runtime.h has not.
+inline int more_dpp(int old, int x, int ctrl, int rows, int banks, bool bound) {
+  const int l = cpu::lane();
+  switch (ctrl) {
+    case 0xB1: return any_lane(x, l ^ 1);
+    case 0x4E: return any_lane(x, l ^ 2);
+    case 0x141: return any_lane(x, l ^ 7);
+    case 0x140: return any_lane(x, l ^ 15);
+  }
+  return cpu::dpp(old, x, ctrl, rows, banks, bound);
+}
+#undef __builtin_amdgcn_update_dpp
+#define __builtin_amdgcn_update_dpp(...) more_dpp(__VA_ARGS__)
+
 // 16 bytes a lane to LDS, zeros from outside the buffer
 struct Buffer {
   const char *base;
