@@ -1,7 +1,7 @@
 // Beam search's choice of continuations, for gfx950:
 //
 // beam_rows   one pass over the logits: of every chunk of 512 tokens the greatest, of
-//             every run of chunks the sum of exponentials
+//             every part of a row the sum of exponentials
 // beam_pick   a workgroup a sequence: ln sum exp of its beams, the n_keep best chunks, and
 //             the n_keep best tokens among those
 //
@@ -15,8 +15,6 @@
 // Beams meet through ln sum exp, and what is chosen are whole numbers, so it is found to about 1e-8:
 // differences to a peak times log2 e in two fp32 steps (the second holds what log2 e as an
 // fp32 lacks), the hardware's exponential (1 ulp), eight of them added in fp32, all else in 64 bits.
-#include <type_traits>
-
 #include "tokens_internal.h"
 
 namespace hermes {
@@ -33,11 +31,11 @@ __device__ __forceinline__ float logit(const void *row, int64_t i) {
   return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t *>(row)[i] << 16);
 }
 
-// Eight logits from i on, -infinity past the last.  (Rows may begin at any element: the
-// loads need no alignment beyond an element's.)
-template <bool FP32>
+// Eight logits from i on, -infinity past the last (Whole: there is none).  Rows may begin at any
+// element: the loads need no alignment beyond an element's.
+template <bool FP32, bool Whole>
 __device__ __forceinline__ void eight(const void *row, int i, int n, float *x) {
-  if (i + 8 <= n) {
+  if (Whole || i + 8 <= n) {
     if constexpr (FP32) {
       __builtin_memcpy(x, static_cast<const float *>(row) + i, 32);
     } else {
@@ -52,47 +50,63 @@ __device__ __forceinline__ void eight(const void *row, int i, int n, float *x) {
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = i + j < n ? logit<FP32>(row, i + j) : -__builtin_inff();
+  for (int j = 0; j < 8; ++j) {
+    const float y = logit<FP32>(row, min(i + j, n - 1));
+    x[j] = i + j < n ? y : -__builtin_inff();
+  }
 }
 
-// Moves between lanes: of 16 lanes, x ^ 1, x ^ 2, 7 - x, 15 - x; then the wave.
-template <int Ctrl>
+// Moves between lanes: of 16 lanes, x ^ 1, x ^ 2, 7 - x, 15 - x, x - 4 and x - 8 around; then the wave.
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kTurn4 = 0x124, kTurn8 = 0x128;
+constexpr int kRow15 = 0x142, kRow31 = 0x143;
+template <int Ctrl, int Rows = 0xF>
 __device__ __forceinline__ int moved(int x) {
-  return __builtin_amdgcn_update_dpp(x, x, Ctrl, 0xF, 0xF, false);
+  return __builtin_amdgcn_update_dpp(0, x, Ctrl, Rows, 0xF, Rows == 0xF);
 }
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRow15 = 0x142, kRow31 = 0x143;
-
-// The greatest of the wave's, in lane 63.
-__device__ __forceinline__ float wave_max(float x) {
-  const auto with = [&](int y) { x = __builtin_fmaxf(x, __builtin_bit_cast(float, y)); };
-  with(moved<kXor1>(__builtin_bit_cast(int, x)));
-  with(moved<kXor2>(__builtin_bit_cast(int, x)));
-  with(moved<kHalfMirror>(__builtin_bit_cast(int, x)));
-  with(moved<kMirror>(__builtin_bit_cast(int, x)));
-  with(moved<kRow15>(__builtin_bit_cast(int, x)));
-  with(moved<kRow31>(__builtin_bit_cast(int, x)));
-  return x;
-}
-
 template <int Ctrl, int Rows = 0xF>
 __device__ __forceinline__ double moved(double x) {
   const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, Ctrl, Rows, 0xF, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), Ctrl, Rows, 0xF, false);
+  const uint32_t lo = moved<Ctrl, Rows>((int)u), hi = moved<Ctrl, Rows>((int)(u >> 32));
   return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
-// The sum of the wave's, in lane 63.
-__device__ __forceinline__ double wave_sum(double x) {
+
+// An int that orders as the float does (NaN apart), and back.
+__device__ __forceinline__ int order_of(float x) {
+  const int u = __builtin_bit_cast(int, x);
+  return u ^ (u >> 31 & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float float_of(int k) { return __builtin_bit_cast(float, k ^ (k >> 31 & 0x7FFFFFFF)); }
+
+template <int Ctrl>
+__device__ __forceinline__ int greater(int x) { return max(x, moved<Ctrl>(x)); }
+// The greatest of the wave's, in all lanes.
+__device__ __forceinline__ int wave_max(int x) {
+  x = greater<kTurn8>(greater<kTurn4>(greater<kXor2>(greater<kXor1>(x))));
+  x = max(x, __shfl_xor(x, 16));
+  return max(x, __shfl_xor(x, 32));
+}
+// Of four values the greatest of the wave's: value l % 4 in lane l.
+__device__ __forceinline__ int wave_max(int a, int b, int c, int d) {
+  const int lane = threadIdx.x & 63;
+  const bool one = lane & 1, two = lane & 2;
+  const int x = max(one ? b : a, moved<kXor1>(one ? a : b)), y = max(one ? d : c, moved<kXor1>(one ? c : d));
+  int z = max(two ? y : x, moved<kXor2>(two ? x : y));
+  z = greater<kTurn8>(greater<kTurn4>(z));
+  z = max(z, __shfl_xor(z, 16));
+  return max(z, __shfl_xor(z, 32));
+}
+
+// The sum of 16 lanes, in all of them; of the wave's, in lane 63.
+__device__ __forceinline__ double row_sum(double x) {
   x += moved<kXor1>(x);
   x += moved<kXor2>(x);
   x += moved<kHalfMirror>(x);
-  x += moved<kMirror>(x);
+  return x + moved<kMirror>(x);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  x = row_sum(x);
   x += moved<kRow15, 0xA>(x);
   return x + moved<kRow31, 0xC>(x);
-}
-
-__device__ __forceinline__ float last_lane(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
 template <bool FP32>
@@ -102,53 +116,75 @@ __device__ __forceinline__ const void *row_of(const BeamArgs &a, int64_t r) {
 
 template <bool FP32>
 __global__ __launch_bounds__(kRowThreads) void beam_rows(BeamArgs a) {
-  const int r = blockIdx.y, lane = threadIdx.x & 63;
-  const int part = blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6);
-  if (part >= a.parts || (a.done != nullptr && a.done[r] != 0)) return;
+  __shared__ double sums[kRowThreads / 64];
+  __shared__ float peaks[kRowThreads / 64];
+  const int r = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (a.done != nullptr && a.done[r] != 0) return;
   const void *row = row_of<FP32>(a, r);
-  const int c1 = min((part + 1) * a.per, a.chunks);
+  const int c0 = min(((int)blockIdx.x * (kRowThreads / 64) + wave) * a.per, a.chunks), c1 = min(c0 + a.per, a.chunks);
   float peak = -__builtin_inff();
   double sum = 0.0;
-  // P chunks at once: their loads and their maxima's moves are independent
-  const auto take = [&](int c, auto number) {
-    constexpr int P = decltype(number)::value;
-    float x[P][8], m[P], all;
-#pragma unroll
-    for (int i = 0; i < P; ++i) eight<FP32>(row, (c + i) * kBeamChunk + 8 * lane, a.n_vocab, x[i]);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      m[i] = x[i][0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) m[i] = __builtin_fmaxf(m[i], x[i][j]);
-      m[i] = wave_max(m[i]);
-      if (lane == 63) a.top[(int64_t)r * a.chunks + c + i] = m[i];
-      all = i == 0 ? m[0] : __builtin_fmaxf(all, m[i]);
-    }
-    all = last_lane(all);
-    if (all > peak) {
-      sum = peak == -__builtin_inff() ? 0.0 : sum * exp((double)peak - (double)all);
-      peak = all;
-    }
-    // (all -infinity so far: against zero, they add nothing)
-    const float base = peak == -__builtin_inff() ? 0.0f : peak;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      float e[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = x[i][j] - base;
-        e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2eHigh, d * kLog2eLow));
-      }
-      sum += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+  float *const top = a.top + (int64_t)r * a.chunks;
+  // The greatest logit so far is `now`: older sums are scaled to it.
+  const auto raise = [&](float now) {
+    if (now > peak) {
+      sum = peak == -__builtin_inff() ? 0.0 : sum * exp((double)peak - (double)now);
+      peak = now;
     }
   };
-  int c = part * a.per;
-  for (; c + 4 <= c1; c += 4) take(c, std::integral_constant<int, 4>{});
-  for (; c < c1; ++c) take(c, std::integral_constant<int, 1>{});
+  const auto greatest = [&](const float (&x)[8]) {
+    float m = x[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) m = __builtin_fmaxf(m, x[j]);
+    return order_of(m);
+  };
+  const auto add = [&](const float (&x)[8]) {
+    // (all -infinity so far: against zero, they add nothing)
+    const float base = peak == -__builtin_inff() ? 0.0f : peak;
+    float e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = x[j] - base;
+      e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2eHigh, d * kLog2eLow));
+    }
+    sum += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+  };
+  const int whole = min(c1, a.n_vocab / kBeamChunk);
+  int c = c0;
+  // four chunks at once: their loads run together, and their maxima's moves are shared
+  for (; c + 4 <= whole; c += 4) {
+    float x[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) eight<FP32, true>(row, (c + i) * kBeamChunk + 8 * lane, a.n_vocab, x[i]);
+    const int m = wave_max(greatest(x[0]), greatest(x[1]), greatest(x[2]), greatest(x[3]));
+    if (lane < 4) top[c + lane] = float_of(m);
+    raise(float_of(__builtin_amdgcn_readfirstlane(greater<kXor2>(greater<kXor1>(m)))));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) add(x[i]);
+  }
+#pragma unroll 1
+  for (; c < c1; ++c) {
+    float x[8];
+    eight<FP32, false>(row, c * kBeamChunk + 8 * lane, a.n_vocab, x);
+    const float m = float_of(__builtin_amdgcn_readfirstlane(wave_max(greatest(x))));
+    if (lane == 0) top[c] = m;
+    raise(m);
+    add(x);
+  }
   sum = wave_sum(sum);
-  if (lane == 63) {
-    a.sum[(int64_t)r * a.parts + part] = sum;
-    a.peak[(int64_t)r * a.parts + part] = peak;
+  if (lane == 63) sums[wave] = sum, peaks[wave] = peak;
+  __syncthreads();
+  if (wave == 0) {          // (four lanes' work, done by all)
+    const float at = peaks[lane % 4];
+    const float all = float_of(greater<kXor2>(greater<kXor1>(order_of(at))));
+    double x = sums[lane % 4];
+    if (at != all) x *= exp((double)at - (double)all);
+    x += moved<kXor1>(x);
+    x += moved<kXor2>(x);
+    if (lane == 0) {
+      a.sum[(int64_t)r * a.parts + blockIdx.x] = x;
+      a.peak[(int64_t)r * a.parts + blockIdx.x] = all;
+    }
   }
 }
 
@@ -158,7 +194,8 @@ __global__ __launch_bounds__(kRowThreads) void beam_rows(BeamArgs a) {
 __device__ __forceinline__ bool before(double v, int i, double w, int j) { return v > w || (v == w && i < j); }
 
 constexpr int kList = 2048, kPickWaves = kPickThreads / 64;
-static_assert(kPickThreads == 64 * 16, "64 groups of 16 threads");
+constexpr int kGroup = kPickThreads / 64;   // threads of a group: 64 groups
+static_assert(kGroup == 8 || kGroup == 16, "reduced by three or four moves");
 
 struct PickShared {
   double offset[kMaxBeams];         // score - ln sum exp; a done beam: its score; -infinity: offers nothing
@@ -169,7 +206,7 @@ struct PickShared {
   double value[kList];
   int32_t index[kList];
   int32_t count;
-  unsigned long long counted;
+  int32_t counted;
   double out_value[kMaxKeep];
   int32_t out_index[kMaxKeep];
 };
@@ -179,16 +216,22 @@ struct Candidate {
   int i;
 };
 template <int Ctrl>
-__device__ __forceinline__ Candidate first_of(const Candidate &x) {
-  const Candidate y{moved<Ctrl>(x.v), moved<Ctrl>(x.i)};
-  return before(y.v, y.i, x.v, x.i) ? y : x;
+__device__ __forceinline__ double greater(double x) { return __builtin_fmax(x, moved<Ctrl>(x)); }
+// The first of a group's, the sum over a group.
+__device__ __forceinline__ Candidate group_first(const Candidate &x) {
+  const double v = greater<kMirror>(greater<kHalfMirror>(greater<kXor2>(greater<kXor1>(x.v))));
+  int i = x.v == v ? x.i : INT32_MAX;
+  i = min(i, moved<kXor1>(i));
+  i = min(i, moved<kXor2>(i));
+  i = min(i, moved<kHalfMirror>(i));
+  return Candidate{v, min(i, moved<kMirror>(i))};
 }
-// The sum over 16 lanes.
-__device__ __forceinline__ int row_sum(int x) {
+__device__ __forceinline__ int group_sum(int x) {
   x += moved<kXor1>(x);
   x += moved<kXor2>(x);
   x += moved<kHalfMirror>(x);
-  return x + moved<kMirror>(x);
+  if constexpr (kGroup == 16) x += moved<kMirror>(x);
+  return x;
 }
 
 // Orders as the value does (-0 and 0 alike).
@@ -197,75 +240,77 @@ __device__ __forceinline__ unsigned long long key_of(double v) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// A set of candidates is a function that calls another with (value, index) of each of this
-// thread's; those of value -infinity do not count.
+// A set of candidates has best(), this thread's first one or one that comes shortly after it, and
+// above(edge, take), which calls take(value, index) of this thread's that may be edge or before it.
+// Candidates of value -infinity do not count.
 
-// How many satisfy `test`.
-template <typename Each, typename Test>
-__device__ __forceinline__ unsigned long long count_of(PickShared &s, const Each &each, Test &&test) {
-  __syncthreads();
-  if (threadIdx.x == 0) s.counted = 0;
-  __syncthreads();
-  unsigned long long mine = 0;
-  each([&](double v, int i) { mine += v > kNone && test(v, i); });
-  if (mine != 0) atomicAdd(&s.counted, mine);
-  __syncthreads();
-  return s.counted;
+// The least logit that an edge asks of a beam, or a little less: values are sums in 64 bits, and most logits
+// are sorted out by one comparison in 32.
+__device__ __forceinline__ float least_logit(double edge, double offset) {
+  const double gap = edge - offset;
+  return edge == kNone ? -__builtin_inff() : (float)(gap - 0x1p-20 * __builtin_fabs(gap) - 0x1p-40 * __builtin_fabs(offset));
 }
 
-// The keep-th candidate, bit by bit.
-template <typename Each>
-__device__ Candidate find_edge(PickShared &s, int keep, const Each &each) {
+// The keep-th candidate, bit by bit: first the greatest value that `keep` candidates reach, then of
+// those that tie the least index up to which there are enough.
+template <typename Set>
+__device__ __forceinline__ Candidate find_edge(PickShared &s, int keep, const Set &set) {
   unsigned long long k = 0;
-  for (int bit = 63; bit >= 0; --bit) {
-    const unsigned long long next = k | 1ull << bit;
-    if (count_of(s, each, [&](double v, int) { return key_of(v) >= next; }) >= (unsigned long long)keep) k = next;
-  }
-  const unsigned long long more = count_of(s, each, [&](double v, int) { return key_of(v) > k; });
-  int last = 0;             // of the candidates that tie, the lowest indexes
-  for (int bit = 30; bit >= 0; --bit) {
-    const int next = last | 1 << bit;
-    if (more + count_of(s, each, [&](double v, int i) { return key_of(v) == k && i < next; }) < (unsigned long long)keep)
-      last = next;
+  int last = 0;
+#pragma unroll 1
+  for (int bit = 63 + 31; bit >= 0; --bit) {
+    const bool ties = bit < 31;
+    const unsigned long long key = ties ? k : k | 1ull << (bit - 31);
+    const int end = last | (ties ? 1 << bit : 0);
+    __syncthreads();
+    if (threadIdx.x == 0) s.counted = 0;
+    __syncthreads();
+    int mine = 0;
+    set.above(kNone, [&](double v, int i) {
+      const unsigned long long u = key_of(v);
+      mine += v > kNone && (ties ? u > key || (u == key && i < end) : u >= key);
+    });
+    if (mine != 0) atomicAdd(&s.counted, mine);
+    __syncthreads();
+    if (ties ? s.counted < keep : s.counted >= keep) {
+      if (ties) last = end; else k = key;
+    }
   }
   return Candidate{__builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k), last};
 }
 
-// The `keep` first candidates, in order, to s.out_value and s.out_index; how many there are.
-//
-// The first of each of 64 groups of candidates: the keep-th of those is a bound that at least
-// `keep` candidates reach, and few more do.  Those are listed, and 16 threads each count the ones
-// before it.  Where more reach the bound than the list holds, the bound is raised to the keep-th
-// candidate itself (whole rows of ties: some 100 us).
-template <typename Each>
-__device__ __forceinline__ int pick(PickShared &s, int keep, const Each &each) {
-  const int tid = threadIdx.x, group = tid / 16, slice = tid % 16;
-  Candidate best{kNone, INT32_MAX};
-  each([&](double v, int i) {
-    if (before(v, i, best.v, best.i)) best = Candidate{v, i};
-  });
-  best = first_of<kXor1>(best);
-  best = first_of<kXor2>(best);
-  best = first_of<kHalfMirror>(best);
-  best = first_of<kMirror>(best);
-  if (tid == 0) s.count = 0;
+// A bound that at least `keep` candidates reach, and few more: of the candidates of 64 groups of threads,
+// the keep-th.
+template <typename Set>
+__device__ __forceinline__ Candidate bound_of(PickShared &s, int keep, const Set &set) {
+  const int tid = threadIdx.x, group = tid / kGroup, slice = tid % kGroup;
+  const Candidate best = group_first(set.best());
   if (slice == 0) s.best_value[group] = best.v, s.best_index[group] = best.i;
   __syncthreads();
   int rank = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int g = slice + 16 * j;
+  for (int j = 0; j < 64 / kGroup; ++j) {
+    const int g = slice + kGroup * j;
     const double v = s.best_value[g];
     const int x = s.best_index[g];
     // (empty groups are alike: they take their place in the line)
     rank += before(v, x, best.v, best.i) || (v == best.v && x == best.i && g < group);
   }
-  rank = row_sum(rank);
+  rank = group_sum(rank);
   if (rank == keep - 1 && slice == 0) s.edge_value = best.v, s.edge_index = best.i;
   __syncthreads();
-  Candidate edge{s.edge_value, s.edge_index};
+  return Candidate{s.edge_value, s.edge_index};
+}
+
+// The `keep` first candidates, in order, to s.out_value and s.out_index; how many there are.  At least
+// `keep` reach the edge (or all do): those that do are listed, and a group of threads each counts the
+// ones before it.  Where they are more than the list holds, the edge is raised to the keep-th
+// candidate itself (rows of ties: some 100 us).  s.count is zero.
+template <typename Set>
+__device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Candidate edge) {
+  const int tid = threadIdx.x, group = tid / kGroup, slice = tid % kGroup;
   for (int round = 0;; ++round) {
-    each([&](double v, int i) {
+    set.above(edge.v, [&](double v, int i) {
       if (v > kNone && !before(edge.v, edge.i, v, i)) {
         const int at = atomicAdd(&s.count, 1);
         if (at < kList) s.value[at] = v, s.index[at] = i;
@@ -273,7 +318,7 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, const Each &each) {
     });
     __syncthreads();
     if (s.count <= kList || round > 0) break;
-    edge = find_edge(s, keep, each);
+    edge = find_edge(s, keep, set);
     __syncthreads();
     if (tid == 0) s.count = 0;
     __syncthreads();
@@ -283,83 +328,161 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, const Each &each) {
     const int c = min(c0 + group, count - 1);
     const Candidate x{s.value[c], s.index[c]};
     int first = 0;
-    for (int o = slice; o < count; o += 16) first += before(s.value[o], s.index[o], x.v, x.i);
-    first = row_sum(first);
+    for (int o = slice; o < count; o += kGroup) first += before(s.value[o], s.index[o], x.v, x.i);
+    first = group_sum(first);
     if (slice == 0 && c0 + group < count && first < keep) s.out_value[first] = x.v, s.out_index[first] = x.i;
   }
   __syncthreads();
   return min(count, keep);
 }
 
+// Chunks, each of the value of its greatest token.  A beam's lie in `share` waves.
+struct Chunks {
+  const PickShared &s;
+  const BeamArgs &a;
+  const float *top;         // of the sequence
+  int wave, lane, share;
+
+  // place(b, offset): a beam with chunks of this wave's; done(...): one that is done, to one of its threads
+  template <typename Place, typename Done>
+  __device__ __forceinline__ void walk(Place &&place, Done &&done) const {
+#pragma unroll 1
+    for (int b = wave / share; b < a.n_beams; b += kPickWaves / share) {
+      const double offset = s.offset[b];
+      if (offset == kNone) continue;
+      if (s.done[b] == 0) {
+        place(b, offset);
+      } else if (wave % share == 0 && lane == 0) {
+        done(offset, b * a.chunks + a.pad_token / kBeamChunk);
+      }
+    }
+  }
+  __device__ __forceinline__ Candidate best() const {
+    Candidate x{kNone, INT32_MAX};
+    const auto with = [&](double v, int i) {
+      if (before(v, i, x.v, x.i)) x = Candidate{v, i};
+    };
+    walk([&](int b, double offset) {
+      const float *from = top + b * a.chunks;
+      float m = -__builtin_inff();
+      int at = 0;
+#pragma unroll 4
+      for (int c = wave % share * 64 + lane; c < a.chunks; c += 64 * share) {
+        const float y = from[c];
+        if (y > m) m = y, at = c;
+      }
+      with(offset + (double)m, b * a.chunks + at);
+    }, with);
+    return x;
+  }
+  template <typename Take>
+  __device__ __forceinline__ void above(double edge, Take &&take) const {
+    walk([&](int b, double offset) {
+      const float *from = top + b * a.chunks;
+      const float least = least_logit(edge, offset);
+#pragma unroll 4
+      for (int c = wave % share * 64 + lane; c < a.chunks; c += 64 * share) {
+        const float y = from[c];
+        if (y >= least) take(offset + (double)y, b * a.chunks + c);
+      }
+    }, take);
+  }
+};
+
+// Tokens of the chosen chunks: a chunk is a group's, of 16 threads, with four times eight neighbours each.
+template <bool FP32>
+struct Tokens {
+  const BeamArgs &a;
+  const void *row;          // of the chunk
+  double offset;            // -infinity: no chunk
+  int first, b, done;       // its first token, its beam, whether that is done
+  float x[4][8];
+
+  __device__ __forceinline__ Tokens(const PickShared &s, const BeamArgs &a_, int64_t row0, int n_chunks) : a(a_) {
+    const int n = threadIdx.x / kGroup;
+    b = n < n_chunks ? s.beam[n] : 0;
+    offset = n < n_chunks ? s.offset[b] : kNone;
+    first = n < n_chunks ? s.token[n] + 8 * (threadIdx.x % kGroup) : 0;
+    done = s.done[b];
+    row = row_of<FP32>(a, row0 + b);
+    if (offset == kNone || done) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) eight<FP32, false>(row, first + 128 * k, a.n_vocab, x[k]);
+  }
+  __device__ __forceinline__ Candidate best() const {
+    if (offset == kNone) return Candidate{kNone, INT32_MAX};
+    if (done) return Candidate{threadIdx.x % kGroup == 0 ? offset : kNone, b * a.n_vocab + a.pad_token};
+    float m = x[0][0];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, x[k][j]);
+    // (it is one of them: not after the last)
+    return Candidate{offset + (double)m, b * a.n_vocab + first + 3 * 128 + 7};
+  }
+  template <typename Take>
+  __device__ __forceinline__ void above(double edge, Take &&take) const {
+    if (offset == kNone) return;
+    if (done) {
+      if (threadIdx.x % kGroup == 0) take(offset, b * a.n_vocab + a.pad_token);
+      return;
+    }
+    const float least = least_logit(edge, offset);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) bits |= x[k][j] >= least ? 1u << (8 * k + j) : 0u;
+    // (few: read again, as registers have no index)
+#pragma unroll 1
+    for (; bits != 0; bits &= bits - 1) {
+      const int j = __builtin_ctz(bits), t = first + j / 8 * 128 + j % 8;
+      if (t < a.n_vocab) take(offset + (double)logit<FP32>(row, t), b * a.n_vocab + t);
+    }
+  }
+};
+
 template <bool FP32>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   __shared__ PickShared s;
   const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row0 = (int64_t)seq * a.n_beams;
-  const float *top = a.top + row0 * a.chunks;
-  // a beam's chunks belong to `share` waves
   int share = kPickWaves;
   while (share > 1 && share * a.n_beams > kPickWaves) share /= 2;
-  const int first_chunk = wave % share * 64 + lane;
-  // (asked for now, so that it is near when the sums are done)
-  const float near = wave / share < a.n_beams && first_chunk < a.chunks ? top[wave / share * a.chunks + first_chunk] : 0.0f;
-  for (int b = wave; b < a.n_beams; b += kPickWaves) {
+  // ln sum exp: 16 lanes a beam, a part each (all lanes go through, for the moves between them)
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.n_beams; b0 += kPickThreads / 16) {
+    const int b = min(b0 + tid / 16, a.n_beams - 1), p = tid % 16;
     const int64_t r = row0 + b;
+    const float at = p < a.parts ? a.peak[r * a.parts + p] : -__builtin_inff();
+    double sum = p < a.parts ? a.sum[r * a.parts + p] : 0.0;
     const double score = a.score[r];
     const int done = a.done != nullptr && a.done[r] != 0;
-    double offset = score;
-    if (!done) {
-      const double *sums = a.sum + r * a.parts;
-      const float *peaks = a.peak + r * a.parts;
-      float peak = -__builtin_inff();
-      for (int p = lane; p < a.parts; p += 64) peak = __builtin_fmaxf(peak, peaks[p]);
-      peak = last_lane(wave_max(peak));
-      double sum = 0.0;     // (a NaN or an infinity of the row makes it a NaN)
-      for (int p = lane; p < a.parts; p += 64) {
-        const double x = sums[p];
-        const float at = peaks[p];
-        sum += at == peak ? x : x * exp((double)at - (double)peak);
-      }
-      offset = score - ((double)peak + log(wave_sum(sum)));
-    }
-    if (lane == 63) {
+    const float peak = float_of(greater<kTurn8>(greater<kTurn4>(greater<kXor2>(greater<kXor1>(order_of(at))))));
+    if (at != peak) sum *= exp((double)at - (double)peak);
+    sum = row_sum(sum);     // (a NaN or an infinity of the row makes it a NaN)
+    const double offset = done ? score : score - ((double)peak + log(sum));
+    if (p == 0) {
       s.offset[b] = __builtin_isfinite(offset) ? offset : kNone;
       s.done[b] = done;
     }
   }
-  asm volatile("" ::"v"(near));
+  if (tid == 0) s.count = 0;
   __syncthreads();
-  const int n_chunks = pick(s, a.n_keep, [&](auto &&take) {
-    for (int b = wave / share; b < a.n_beams; b += kPickWaves / share) {
-      const double offset = s.offset[b];
-      if (offset == kNone) continue;
-      if (s.done[b]) {
-        if (first_chunk == 0) take(offset, b * a.chunks + a.pad_token / kBeamChunk);
-        continue;
-      }
-      for (int c = first_chunk; c < a.chunks; c += 64 * share) take(offset + (double)top[b * a.chunks + c], b * a.chunks + c);
-    }
-  });
+  const Chunks chunks{s, a, a.top + row0 * a.chunks, wave, lane, share};
+  const int n_chunks = pick(s, a.n_keep, chunks, bound_of(s, a.n_keep, chunks));
   if (tid < n_chunks) {
     const int i = s.out_index[tid], b = i / a.chunks;
     s.beam[tid] = b;
     s.token[tid] = (i - b * a.chunks) * kBeamChunk;
   }
+  // Each chosen chunk has a token of its value: with n_keep of them, that of the last is a bound.
+  Candidate edge{s.out_value[a.n_keep - 1], INT32_MAX};
+  if (tid == 0) s.count = 0;
   __syncthreads();
-  const int n = pick(s, a.n_keep, [&](auto &&take) {
-    for (int k = wave; k < n_chunks; k += kPickWaves) {
-      const int b = s.beam[k], t = s.token[k] + 8 * lane;
-      const double offset = s.offset[b];
-      if (s.done[b]) {
-        if (lane == 0) take(offset, b * a.n_vocab + a.pad_token);
-        continue;
-      }
-      float x[8];
-      eight<FP32>(row_of<FP32>(a, row0 + b), t, a.n_vocab, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) take(offset + (double)x[j], b * a.n_vocab + t + j);
-    }
-  });
+  const Tokens<FP32> tokens(s, a, row0, n_chunks);
+  if (n_chunks < a.n_keep) edge = bound_of(s, a.n_keep, tokens);
+  const int n = pick(s, a.n_keep, tokens, edge);
   if (tid < a.n_keep) {
     const bool some = tid < n;
     const int x = some ? s.out_index[tid] : 0, b = x / a.n_vocab, t = x - b * a.n_vocab;
@@ -374,7 +497,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 }  // namespace
 
 hipError_t launch_beam_select(const BeamArgs &a, bool fp32, hipStream_t s) {
-  const dim3 rows((a.parts + kRowThreads / 64 - 1) / (kRowThreads / 64), a.n_seqs * a.n_beams), one(a.n_seqs);
+  const dim3 rows(a.parts, a.n_seqs * a.n_beams), one(a.n_seqs);
   if (fp32) {
     hipLaunchKernelGGL((beam_rows<true>), rows, dim3(kRowThreads), 0, s, a);
     hipLaunchKernelGGL((beam_pick<true>), one, dim3(kPickThreads), 0, s, a);

@@ -73,13 +73,14 @@ int check_beams(const hermes_beam_config *c) {
   return HERMES_OK;
 }
 
-// Rows' waves take so many chunks that some thousands of waves are left.
+// A wave takes so many chunks of a row that some thousands of waves are left, and a row has 16 parts, of
+// four waves, at most.
 void cut_of(const hermes_beam_config *c, BeamArgs *a) {
   const int64_t rows = (int64_t)c->n_seqs * c->n_beams;
   a->chunks = (int32_t)over(c->n_vocab, kBeamChunk);
-  const int64_t per = rows * a->chunks / 8192;
-  a->per = (int32_t)(per < 1 ? 1 : per > 16 ? 16 : per);
-  a->parts = (int32_t)over(a->chunks, a->per);
+  const int64_t even = rows * a->chunks / 32768, least = over(a->chunks, 64), per = even < 16 ? even : 16;
+  a->per = (int32_t)(per > least ? per : least);
+  a->parts = (int32_t)over(a->chunks, 4 * a->per);
 }
 
 struct BeamRoom { int64_t sum, peak, top, all; };

@@ -51,7 +51,7 @@ struct BeamArgs {
   int64_t stride;
   int32_t n_seqs, n_beams, n_vocab, n_keep, end_token, pad_token;
   int32_t chunks;           // of a row
-  int32_t per, parts;       // chunks of a wave, waves of a row
+  int32_t per, parts;       // chunks of a wave; parts of a row, of four waves (16 at most)
   float *top;               // [rows][chunks]: a chunk's greatest logit
   double *sum;              // [rows][parts]: sum of exp(logit - peak)
   float *peak;              // [rows][parts]

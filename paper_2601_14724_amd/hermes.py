@@ -696,33 +696,39 @@ def beam_select(logits: torch.Tensor, score: torch.Tensor, keep: int, done: Opti
     if not isinstance(logits, torch.Tensor) or logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("logits: expected torch.bfloat16 or torch.float32 [n_seqs][n_beams][n_vocab]")
     n_seqs, n_beams, n_vocab = logits.shape
-    if not logits.is_cuda:
+    index = logits.get_device()
+    if index < 0:
         raise ValueError("logits: must be a device tensor")
     ss, stride, es = logits.stride()
-    if n_beams == 1 or logits.numel() == 0:
-        stride = ss
     if logits.numel() == 0 or n_seqs * n_beams == 1:
         stride = max(n_vocab, 1)
+    elif n_beams == 1:
+        stride = ss
     elif n_seqs > 1 and ss != n_beams * stride:
         raise ValueError("logits: rows must lie evenly apart")
     if es != 1 and n_vocab > 1:
         raise ValueError("logits: a row must be contiguous")
-    for t, dtype, name in ((score, torch.float32, "score"), (done, torch.int32, "done")):
-        if t is None and name == "done":
-            continue
-        _need(t, dtype, (n_seqs, n_beams), name)
-        if t.device != logits.device:
-            raise ValueError(f"{name}: a tensor on {t.device}, the logits are on {logits.device}")
+    _beams_of(score, torch.float32, (n_seqs, n_beams), index, "score")
+    if done is not None:
+        _beams_of(done, torch.int32, (n_seqs, n_beams), index, "done")
     cfg = BeamConfig(n_seqs, n_beams, n_vocab, keep, FP32 if logits.dtype is torch.float32 else BF16, end_token, pad_token)
-    nbytes = lib.hermes_beam_workspace_bytes(ctypes.byref(cfg))
+    ref = ctypes.byref(cfg)
+    nbytes = lib.hermes_beam_workspace_bytes(ref)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-    out = torch.empty((4, n_seqs, max(keep, 0)), dtype=torch.int32, device=logits.device)
-    best, parent, token, ended = out.unbind(0)
-    best = best.view(torch.float32)
-    _on(logits.get_device(), lib.hermes_beam_select, "hermes_beam_select", ctypes.byref(cfg), logits.data_ptr(), stride,
-        score.data_ptr(), _ptr(done), best.data_ptr(), parent.data_ptr(), token.data_ptr(), ended.data_ptr(),
-        ws.data_ptr(), nbytes)
+    shape = (n_seqs, max(keep, 0))
+    best = torch.empty(shape, dtype=torch.float32, device=logits.device)
+    parent, token, ended = torch.empty((3,) + shape, dtype=torch.int32, device=logits.device).unbind(0)
+    _on(index, lib.hermes_beam_select, "hermes_beam_select", ref, logits.data_ptr(), stride, score.data_ptr(), _ptr(done),
+        best.data_ptr(), parent.data_ptr(), token.data_ptr(), ended.data_ptr(), ws.data_ptr(), nbytes)
     return best, parent, token, ended
+
+
+def _beams_of(t: torch.Tensor, dtype: torch.dtype, shape: tuple, index: int, name: str) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {dtype} {shape}, got {getattr(t, 'dtype', None)} "
+                         f"{tuple(getattr(t, 'shape', ()))}")
+    if t.get_device() != index:
+        raise ValueError(f"{name}: a tensor on {t.device}, the logits are on device {index}")
 
 
 class PackedWeight:
@@ -758,25 +764,41 @@ class PackedWeight:
                              f"{tuple(getattr(x, 'shape', ()))}")
         n = x.shape[0]
         shape = (n, self.n_out)
+        self._on_device(x, "x")
+        bp = ap = None
+        if bias is not None:
+            self._fits(bias, torch.bfloat16, (self.n_out,), "bias")
+            bp = bias.data_ptr()
+        if add is not None:
+            self._fits(add, torch.bfloat16, shape, "add")
+            ap = add.data_ptr()
+        if out is not None:
+            dtype = out.dtype if isinstance(out, torch.Tensor) else dtype
+        kind = FP32 if dtype is torch.float32 else BF16
+        if kind == BF16 and dtype is not torch.bfloat16:
+            raise ValueError(f"dtype: torch.bfloat16 or torch.float32, got {dtype}")
         if out is None:
-            if dtype is not torch.bfloat16 and dtype is not torch.float32:
-                raise ValueError("dtype: torch.bfloat16 or torch.float32")
             out = torch.empty(shape, dtype=dtype, device=self.device)
-        elif not isinstance(out, torch.Tensor) or out.dtype not in (torch.bfloat16, torch.float32):
-            raise ValueError("out: expected torch.bfloat16 or torch.float32")
-        for t, want, type_, name in ((bias, (self.n_out,), torch.bfloat16, "bias"), (add, shape, torch.bfloat16, "add"),
-                                     (out, shape, out.dtype, "out")):
-            if t is not None and (t.dtype is not type_ or t.shape != want or not t.is_contiguous()):
-                raise ValueError(f"{name}: expected contiguous {type_} {want}, got {t.dtype} {tuple(t.shape)}")
-        for t in (x, bias, add, out):
-            if t is not None and t.get_device() != self._index:
-                raise ValueError(f"product: a tensor on {t.device}, the weight is on {self.device}")
-        if n and x.stride(1) != 1 and self.n_in > 1:
+        else:
+            self._fits(out, dtype, shape, "out")
+        stride, es = x.stride()
+        if n <= 1:
+            stride = -(-self.n_in // 8) * 8
+        if es != 1 and self.n_in > 1 and n:
             raise ValueError("x: a row must be contiguous")
-        stride = x.stride(0) if n > 1 else -(-self.n_in // 8) * 8
-        _on(self._index, lib.hermes_weight_product, "hermes_weight_product", self._ref, x.data_ptr(), stride, n, _ptr(bias),
-            _ptr(add), out.data_ptr(), FP32 if out.dtype is torch.float32 else BF16)
+        _on(self._index, lib.hermes_weight_product, "hermes_weight_product", self._ref, x.data_ptr(), stride, n, bp, ap,
+            out.data_ptr(), kind)
         return out
+
+    def _on_device(self, t: torch.Tensor, name: str) -> None:
+        if t.get_device() != self._index:
+            raise ValueError(f"{name}: a tensor on {t.device}, the weight is on {self.device}")
+
+    def _fits(self, t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> None:
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous {dtype} {shape}, got {getattr(t, 'dtype', None)} "
+                             f"{tuple(getattr(t, 'shape', ()))}")
+        self._on_device(t, name)
 
 
 def default_sm_scale(head_dim: int) -> float:

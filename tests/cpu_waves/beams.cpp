@@ -19,7 +19,7 @@ int main(int, char **argv) {
   a.pad_token = number(8);
   a.per = number(10);
   a.chunks = (a.n_vocab + kBeamChunk - 1) / kBeamChunk;
-  a.parts = (a.chunks + a.per - 1) / a.per;
+  a.parts = (a.chunks + 4 * a.per - 1) / (4 * a.per);
   const size_t rows = (size_t)a.n_seqs * a.n_beams, n = (rows - 1) * a.stride + a.n_vocab, k = (size_t)a.n_seqs * a.n_keep;
   a.logits = fp32 ? static_cast<const void *>(input<float>(n)) : input<uint16_t>(n);
   a.score = input<float>(rows);

@@ -33,6 +33,8 @@ inline int more_dpp(int old, int x, int ctrl, int rows, int banks, bool bound) {
   switch (ctrl) {
     case 0xB1: return any_lane(x, l ^ 1);
     case 0x4E: return any_lane(x, l ^ 2);
+    case 0x124: return any_lane(x, (l & ~15) | ((l - 4) & 15));
+    case 0x128: return any_lane(x, (l & ~15) | ((l - 8) & 15));
     case 0x141: return any_lane(x, l ^ 7);
     case 0x140: return any_lane(x, l ^ 15);
   }
