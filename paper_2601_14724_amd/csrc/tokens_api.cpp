@@ -230,7 +230,11 @@ int hermes_page_reorder(const hermes_page_pool *pool, const hermes_page_beams *b
   const bool fp4 = pool->format == HERMES_PAGE_FP4;
   a.row_bytes = fp4 ? pool->head_dim / 2 : 2 * pool->head_dim;
   a.scale_bytes = fp4 ? pool->head_dim / 32 : 0;
-  const int64_t shares = kStreamSlots / b->n_groups;
+  // A group's copies, about a third of its beams' pages, are shared by workgroups as far as all are on the
+  // device at once, for 64 KiB of pages each (28 layers of eight sequences, eight beams of 34 KiB pages: 15.2 us with
+  // one, 12.3 with four; of 16 sequences 22.5, and 18.0 with two; one layer of eight 10.7, and 6.6 with five).
+  const int64_t room = 4 * kStreamSlots / b->n_groups, use = over(b->n_beams * a.pool.page_bytes, 1 << 16);
+  const int64_t shares = room < use ? room : use;
   a.shares = (int32_t)(shares < 1 ? 1 : shares > 8 ? 8 : shares);
   return launch_page_reorder(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
 }
