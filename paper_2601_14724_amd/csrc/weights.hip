@@ -79,12 +79,10 @@ __device__ __forceinline__ bf16x8 unpack(uint32_t codes, float scale) {
 // Inputs k .. k + 7 of a row, zeros past the last.
 __device__ __forceinline__ u32x4 inputs(const uint16_t *row, int k, int n_in) {
   if (k + 8 <= n_in) return *reinterpret_cast<const u32x4 *>(row + k);
-  u32x4 v;
+  u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = k + 2 * i < n_in ? row[k + 2 * i] : 0u, hi = k + 2 * i + 1 < n_in ? row[k + 2 * i + 1] : 0u;
-    v[i] = lo | hi << 16;
-  }
+  for (int i = 0; i < 8; ++i)
+    if (k + i < n_in) v[i / 2] |= (uint32_t)row[k + i] << (i % 2 * 16);
   return v;
 }
 
@@ -167,7 +165,6 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   const int nt0 = (blockIdx.x * (W / split) + wave / split) * NT;
   const int q = lane / 16, n16 = lane % 16, r0 = blockIdx.y * 16 * MT;
   const int k0 = (int)((int64_t)a.w.tiles_in * sub / split), k1 = (int)((int64_t)a.w.tiles_in * (sub + 1) / split);
-  const int whole = a.w.n_in / 128;
   const int rows = min(a.n_rows - r0, 16 * MT);
   // (an offset in the rows of a block stays below 2^32: 64 rows of up to 2^24 elements)
   const uint16_t *x0 = a.x + (int64_t)r0 * a.x_stride;
@@ -195,27 +192,10 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  const auto load = [&](Step<NT, U> &s, int kt, int slot) {
+  const auto weights = [&](Step<NT, U> &s, int kt, int end) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (kt + i >= k1) break;
-      uint8_t *to = mine + slot * kSlot + i * kTile;
-      if (kt + i < whole) {
-#pragma unroll
-        for (int r = 0; r < RQ; ++r)
-          load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
-      } else {
-#pragma unroll
-        for (int r = 0; r < RQ; ++r) {
-          const int row = min(4 * r + q, rows - 1);
-          *reinterpret_cast<u32x4 *>(to + r * 1024 + lane * 16) =
-              inputs(x0 + row * a.x_stride, 128 * (kt + i) + 8 * (n16 ^ ((4 * r + q) % 16)), a.w.n_in);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (kt + i >= k1) break;
+      if (kt + i >= end) break;
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
         s.codes[i][u] = *reinterpret_cast<const u32x4 *>(codes[u] + (int64_t)(kt + i) * 1024);
@@ -223,10 +203,19 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
       }
     }
   };
-  const auto multiply = [&](const Step<NT, U> &s, int kt, int slot) {
+  const auto load = [&](Step<NT, U> &s, int kt, int end, int slot) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (kt + i >= k1) break;
+      if (kt + i >= end) break;
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, mine + slot * kSlot + i * kTile + r * 1024);
+    }
+    weights(s, kt, end);
+  };
+  const auto multiply = [&](const Step<NT, U> &s, int kt, int end, int slot) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (kt + i >= end) break;
       const uint8_t *tile = mine + slot * kSlot + i * kTile;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -242,28 +231,29 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
       }
     }
   };
-  if (nt0 < a.w.tiles_out && k0 < k1) {
-    Step<NT, U> even, odd;
-    load(even, k0, 0);
-    for (int kt = k0; kt < k1; kt += 2 * U) {
+  if (nt0 < a.w.tiles_out) {
+    const int end = min(k1, a.w.n_in / 128);            // of the whole tiles
+    Step<NT, U> now, next;
+    int slot = 0;
+    if (k0 < end) load(now, k0, end, 0);
+#pragma unroll 1
+    for (int kt = k0; kt < end; kt += U) {
       wait_for_loads();
-      if (kt + U < k1) load(odd, kt + U, 1);
-      multiply(even, kt, 0);
-      if (kt + U >= k1) break;
-      wait_for_loads();
-      if (kt + 2 * U < k1) load(even, kt + 2 * U, 0);
-      multiply(odd, kt + U, 1);
+      if (kt + U < end) load(next, kt + U, end, slot ^ 1);
+      multiply(now, kt, end, slot);
+      now = next;
+      slot ^= 1;
     }
-  }
-  if (split == 1) {
-#pragma unroll
-    for (int u = 0; u < NT; ++u)
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const int r = 16 * t + n16;
-        if (nt0 + u < a.w.tiles_out && r < rows) store(a, r0 + r, 16 * (nt0 + u) + 4 * q, acc[u][t]);
-      }
-    return;
+    if (end < k1) {         // the last tile, in part past the inputs
+      wait_for_loads();
+#pragma unroll 1
+      for (int r = 0; r < RQ; ++r)
+        *reinterpret_cast<u32x4 *>(mine + r * 1024 + lane * 16) =
+            inputs(x0 + min(4 * r + q, rows - 1) * a.x_stride, 128 * end + 8 * (n16 ^ ((4 * r + q) % 16)), a.w.n_in);
+      weights(now, end, k1);
+      wait_for_loads();
+      multiply(now, end, k1, 0);
+    }
   }
   __syncthreads();
   f32x4 *part = reinterpret_cast<f32x4 *>(room);        // [waves][NT MT][64]
@@ -274,10 +264,12 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   __syncthreads();
   // tile i of group g: summed over the group's waves, in their order
   const int groups = W / split;
+#pragma unroll 1
   for (int i = wave; i < groups * NT * MT; i += W) {
     const int g = i / (NT * MT), tile = i % (NT * MT);
     const int nt = (blockIdx.x * groups + g) * NT + tile / MT, r = 16 * (tile % MT) + n16;
     f32x4 v = part[(g * split * MT * NT + tile) * 64 + lane];
+#pragma unroll 1
     for (int s = 1; s < split; ++s) v += part[((g * split + s) * MT * NT + tile) * 64 + lane];
     if (nt < a.w.tiles_out && r < rows) store(a, r0 + r, 16 * nt + 4 * q, v);
   }
