@@ -42,13 +42,19 @@ __global__ __launch_bounds__(256) void weight_pack(WeightPackArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int k0 = 128 * kt + 32 * j + 8 * q, have = n < a.w.n_out ? a.w.n_in - k0 : 0;
-      uint32_t v[4], m = 0;
+      uint32_t v[4] = {0, 0, 0, 0}, m = 0;
+      if (have >= 8) {
+        __builtin_memcpy(v, row + k0, 16);      // (a row may begin at any element)
+      } else {
+#pragma unroll 1
+        for (int x = 0; x < have; ++x) {
+          const uint32_t bits = (uint32_t)row[k0 + x] << (x % 2 * 16);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint32_t lo = 2 * x < have ? row[k0 + 2 * x] : 0u, hi = 2 * x + 1 < have ? row[k0 + 2 * x + 1] : 0u;
-        v[x] = lo | hi << 16;
-        m = max(m, max(lo & 0x7FFFu, hi & 0x7FFFu));
+          for (int y = 0; y < 4; ++y) v[y] |= x / 2 == y ? bits : 0u;
+        }
       }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) m = max(m, max(v[x] & 0x7FFFu, v[x] >> 16 & 0x7FFFu));
       m = max(m, (uint32_t)__shfl_xor((int)m, 16));
       m = max(m, (uint32_t)__shfl_xor((int)m, 32));
       const uint32_t scale = m >= 0x7F80u ? 255u : (uint32_t)min(max((int)((m + 31u) >> 7) - 2, 127 - 119), 127 + 125);
