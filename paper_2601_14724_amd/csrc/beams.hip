@@ -12,9 +12,17 @@
 // beam or token: K tokens before t.  So the pass over the logits keeps nothing but maxima and sums,
 // and is bound by HBM, whatever the logits are.
 //
-// Beams meet through ln sum exp, and what is chosen are whole numbers, so it is found to about 1e-8:
-// differences to a peak times log2 e in two fp32 steps (the second holds what log2 e as an
+// Beams meet through ln sum exp, and what is chosen are whole numbers, so it is found closer than in fp32:
+// differences to the greatest logit times log2 e in two fp32 steps (the second holds what log2 e as an
 // fp32 lacks), the hardware's exponential (1 ulp), eight of them added in fp32, all else in 64 bits.
+// Term by term that is 1e-6 at worst (an argument of 16 octaves and more has half an ulp of 2^-20), which
+// logits that differ average out: 1e-8.
+//
+// Measured: 16 sequences of eight beams over 131072 tokens in bf16, 34 MB, 9.7 us (85 vector instructions
+// for 512 logits a wave, the exponentials four of them each: as much as HBM's rate allows) and 9.7 for the choice;
+// 32 of 16 in fp32, 268 MB, 44 us (6.1 TB/s; part of it stays in the Infinity Cache) and 12.8.  The choice is a
+// workgroup a sequence, a chain of loads, moves and barriers: 7.7 us where it is short.  Its code is kept
+// small: it runs once, so that every line is fetched (62 KB of unrolled loops took 8.7 us for 7.3).
 #include "tokens_internal.h"
 
 namespace hermes {

@@ -12,7 +12,7 @@ import torch
 from oracle import pages_oracle as pages
 from oracle import tokens_oracle as orc
 from paper_2601_14724_amd import hermes as H
-from tests.test_tokens_bounds import beams_of, check_choice
+from tests.test_tokens_bounds import DOUBT, beams_of, check_choice
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -135,6 +135,54 @@ def test_a_weight_s_columns_come_back_exactly():
     assert torch.isnan(got[7]).all() and not torch.isnan(got[:7]).any() and not torch.isnan(got[8:]).any()
 
 
+def test_a_block_with_an_infinity_makes_its_output_nan():
+    wb = weight_bits(40, 300, 6)
+    wb[7, 130], wb[33, 299] = 0x7F80, 0x7FC0
+    x = torch.randn(3, 304, device=DEV).to(torch.bfloat16)[:, :300]
+    bad = torch.isnan(H.PackedWeight(bf16(wb)).product(x))
+    assert bad[:, [7, 33]].all() and bad.sum() == 6
+
+
+def test_an_infinite_input_does_as_the_sum_does():
+    """(padded inputs and other tiles add nothing to it)"""
+    wb = np.zeros((20, 140), np.uint16)
+    wb[:, 139] = pages.bf16_bits(np.arange(20) % 3 - 1.0)
+    x = torch.zeros(2, 144, dtype=torch.bfloat16, device=DEV)[:, :140]
+    x[1, 139] = float("inf")
+    got = H.PackedWeight(bf16(wb)).product(x, dtype=torch.float32).cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = np.float32(np.inf) * (np.arange(20) % 3 - 1.0).astype(np.float32)
+    assert (got[0] == 0).all() and np.array_equal(got[1], want, equal_nan=True)
+
+
+def test_the_same_call_gives_the_same_bits():
+    w = H.PackedWeight(bf16(weight_bits(5000, 1000, 7)))
+    x = torch.randn(33, 1000, device=DEV).to(torch.bfloat16)
+    first = w.product(x, dtype=torch.float32)
+    logits = first.view(3, 11, 5000)
+    chosen = H.beam_select(logits, torch.zeros(3, 11, device=DEV), 22)
+    for _ in range(5):
+        assert torch.equal(w.product(x, dtype=torch.float32), first)
+        assert all(torch.equal(a, b) for a, b in zip(H.beam_select(logits, torch.zeros(3, 11, device=DEV), 22), chosen))
+
+
+def test_a_weight_of_more_than_4_gib():
+    """Its last outputs, whose codes and scales lie past 2^32 bytes; the others are zeros."""
+    n, k = 2 ** 21 + 19, 4224
+    dense = torch.zeros(n, k, dtype=torch.bfloat16, device=DEV)
+    wb = weight_bits(40, k, 8)
+    dense[-40:] = bf16(wb)
+    w = H.PackedWeight(dense)
+    del dense
+    assert w.data.numel() > 2 ** 32
+    xb = pages.bf16_bits(np.random.default_rng(9).standard_normal((2, k)))
+    got = w.product(bf16(xb), dtype=torch.float32)
+    assert (got[:, :-40] == 0).all()
+    want, mag = orc.product(pages.bf16_value(xb), orc.weight(wb))
+    err = np.abs(got[:, -40:].double().cpu().numpy() - want)
+    assert (err <= (k + 2) * 2.0 ** -23 * mag + 2.0 ** -24 * np.abs(want)).all()
+
+
 def test_a_product_writes_its_outputs_only():
     w = H.PackedWeight(bf16(weight_bits(37, 100, 2)))
     for kind in (torch.bfloat16, torch.float32):
@@ -243,14 +291,44 @@ def test_masked_tokens_and_rows_that_offer_nothing():
     assert set(got[1][2]) <= {0, 1, 3, 4}
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("allowed", [0, 5])
+def test_tokens_masked_by_the_lowest_value(kind, allowed):
+    """Finite, so they are chosen where nothing else is left: whole rows of ties."""
+    lowest = float(torch.finfo(torch.bfloat16 if kind == "bf16" else torch.float32).min)
+    x = np.full((2, 3, 40000), lowest, np.float32)
+    rng = np.random.default_rng(5)
+    for i in range(allowed):
+        x[:, :, 7000 * i + 11] = pages.bf16_value(pages.bf16_bits(rng.standard_normal((2, 3)))).astype(np.float32)
+    got = H.beam_select(device_logits(x, kind), torch.tensor([[0.0, -1, -2]] * 2, device=DEV), 32)
+    parent, token = got[1].cpu().numpy(), got[2].cpu().numpy()
+    free = [7000 * i + 11 for i in range(allowed)]
+    for s in range(2):
+        best = sorted(zip(parent[s, :3 * allowed], token[s, :3 * allowed]))
+        assert best == [(b, t) for b in range(3) for t in free]
+        # (a value of that size is the same for all tokens of the lowest logit, of every beam)
+        rest = [t for t in range(40) if t not in free][:32 - 3 * allowed]
+        assert (parent[s, 3 * allowed:] == 0).all() and token[s, 3 * allowed:].tolist() == rest
+
+
+def test_rows_that_lie_gibibytes_apart():
+    stride = 2 ** 30 + 24
+    room = torch.empty(3 * stride + 1000, dtype=torch.bfloat16, device=DEV)
+    rows = room.as_strided((2, 2, 1000), (2 * stride, stride, 1))
+    x = logits_of(np.random.default_rng(6), 2, 2, 1000, "bf16")
+    rows.copy_(torch.from_numpy(x).to(DEV))
+    got = [t.cpu().numpy() for t in H.beam_select(rows, torch.zeros(2, 2, device=DEV), 5)]
+    check_choice(x, np.zeros((2, 2), np.float32), None, 5, -1, 0, got)
+
+
 def test_choices_of_few_tokens_leave_no_rest():
     got = choose(np.float32([[[1, 2, 3], [3, 2, 1]]]), np.zeros((1, 2), np.float32), 9, "fp32", end=0)
     assert got[1][0].tolist() == [0, 1, 0, 1, 0, 1, -1, -1, -1] and got[2][0].tolist() == [2, 0, 1, 1, 0, 2, -1, -1, -1]
     assert got[3][0].tolist() == [0, 1, 0, 0, 1, 0, 0, 0, 0]
 
 
-def test_a_peak_far_from_the_first_tokens_keeps_the_sum_exact():
-    """ln sum exp to 1e-8: what beams are compared through (here a flat row after a steep one)."""
+def test_scores_of_steep_and_flat_rows():
+    """ln sum exp where a peak comes late, where two values are all that a row holds, and where it rises slowly."""
     for kind in ("bf16", "fp32"):
         x = np.zeros((1, 2, 131072), np.float32)
         x[0, 0, ::2] = -5
@@ -265,9 +343,9 @@ def test_a_peak_far_from_the_first_tokens_keeps_the_sum_exact():
             lse = row.max() + np.log(np.exp(row - row.max()).sum())
             mine = (got[1][0] == b).nonzero()[:, 0]
             for i in mine.tolist():
-                # rounded once to fp32: half a step of it, and 1e-8
+                # rounded once to fp32: half a step of it
                 true = row[int(got[2][0, i])] - lse
-                assert abs(float(got[0][0, i]) - true) <= 2.0 ** -24 * abs(true) + 1e-8
+                assert abs(float(got[0][0, i]) - true) <= 2.0 ** -24 * abs(true) + DOUBT
 
 
 def test_strides_that_are_no_rows_are_refused():
@@ -335,6 +413,18 @@ def test_a_shared_prompt_is_forked_without_writing_to_it():
     for t in (6, 7, 8, 9):
         orc.copy_rows(memory, 2, 64, 16, "fp4", 2, t, 8)
     assert (pool.pages.cpu().numpy() == memory).all()
+
+
+def test_pages_past_4_gib_are_copied():
+    n_pages = 2 ** 32 // (4 * pages.block_bytes(128, 64, "fp4")) + 40
+    pool = H.KVPages(4, 4, 128, n_pages, page_rows=64)
+    pool.pages[-30:] = torch.randint(0, 255, (30, pool.page_bytes), dtype=torch.uint8, device=DEV)
+    memory = pool.pages[-30:].cpu().numpy()
+    first = n_pages - 30
+    out, _ = pool.reorder(i32([[[first + 3], [first + 4]]]), i32([[50, 41]]), i32([[1, 1]]), i32([[first, 20]]))
+    assert out.tolist() == [[[first + 4], [first]]] and pool.faults() == 0
+    orc.copy_rows(memory, 4, 128, 64, "fp4", 4, 0, 44)
+    assert (pool.pages[-30:].cpu().numpy() == memory).all()
 
 
 def test_reorder_refuses_other_tensors():
@@ -451,8 +541,8 @@ def test_beams_hold_what_their_own_tokens_alone_would_have_stored(seqs, beams, f
             start = torch.arange(0, n * m.n + 1, n, dtype=torch.int32, device=DEV)
             rows.append(pool.read(H.PageBatch(tab[i].flatten(0, 1), lens[i].reshape(-1), start, n_rows=n * m.n)))
         assert torch.equal(rows[0][0], rows[1][0]) and torch.equal(rows[0][1], rows[1][1])
-    # a score is rounded to fp32 a step, and each step's value found to 1e-7
-    bound = steps * (2.0 ** -24 * float(total.abs().max()) + 1e-7)
+    # a score is rounded to fp32 at each step
+    bound = steps * (2.0 ** -24 * float(total.abs().max()) + DOUBT)
     assert (total - score.double().cpu()).abs().max() <= bound
 
 

@@ -93,7 +93,13 @@ def beams(tmp_path_factory):
     return compiled(tmp_path_factory, "beams", "-O1")
 
 
-def check_choice(logits, score, done, keep, end, pad, got, doubt=1e-7):
+# ln sum exp, term by term relative to its exponential: one ulp of the hardware's exponential (2^-23), half an
+# ulp of its argument (2^-21 below 16 octaves, 2^-20 below 32: what lies further down adds less than 2^-11 of a
+# row of 2^20), times ln 2, and three additions in fp32 (3 x 2^-24): 9.6e-7.
+DOUBT = 1e-6
+
+
+def check_choice(logits, score, done, keep, end, pad, got, doubt=DOUBT):
     """got (score, parent, token, done) [seqs][keep] of logits [seqs][beams][vocab] against the
     definition.  Where two values differ by less than `doubt` either order passes."""
     for s in range(logits.shape[0]):
@@ -105,7 +111,7 @@ def check_choice(logits, score, done, keep, end, pad, got, doubt=1e-7):
         assert (g_done[n:] == 0).all()
         mine = value[g_parent[:n], g_token[:n]]
         assert (np.abs(mine - want) <= doubt).all()
-        # a score is a value rounded once, found to 1e-7
+        # a score is a value rounded once
         assert (np.abs(g_score[:n].astype(np.float64) - mine) <= doubt + 2.0 ** -24 * np.abs(mine)).all()
         assert len({*zip(g_parent[:n].tolist(), g_token[:n].tolist())}) == n
         flat = np.sort(value.reshape(-1))[::-1][:keep + 1]
