@@ -725,11 +725,18 @@ int hermes_weight_pack(const hermes_weight *w, const void *dense, int64_t stride
  *  add          device bf16 [n_rows][n_out], or NULL; may be out, where that is bf16.
  *  out          device [n_rows][n_out] of out_type HERMES_BF16 or HERMES_FP32, 16-byte aligned, apart
  *               from x.
- * Runs on `stream` of the current device, allocates nothing, keeps nothing, and never synchronises.
- * Errors: EINVAL, EHIP.
+ *  workspace    device memory of hermes_weight_workspace_bytes, 16-byte aligned, apart from all of them (may
+ *               be NULL if that is 0); free again when the call's work is done.
+ * Runs on `stream` of the current device, allocates nothing, keeps nothing, and never synchronises; calls
+ * at once need a workspace each.
+ * Errors: EINVAL, ECAPACITY (workspace too small), EHIP.
  */
 int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_stride, int32_t n_rows,
-                          const void *bias, const void *add, void *out, int32_t out_type, void *stream);
+                          const void *bias, const void *add, void *out, int32_t out_type, void *workspace,
+                          size_t ws_bytes, void *stream);
+
+/* Bytes of workspace that a product of n_rows rows needs (0: none, or bad sizes). */
+size_t hermes_weight_workspace_bytes(const hermes_weight *w, int32_t n_rows);
 
 #ifdef __cplusplus
 }

@@ -40,14 +40,27 @@ int64_t bytes_of(const WeightView &v) {
   return (int64_t)v.tiles_out * v.tiles_in * 1024 + (int64_t)v.tiles_out * v.quads * 256;
 }
 
-// The cut of a product.  Fitted to 255 sizes (1, 8, 16, 32 and 64 rows, 64 to 131072 outputs, 128 to 14336
-// inputs), each with every cut: on average 1.5 to 3% slower than the best one.  More tiles a wave
-// read x less often (64 rows on 14336 x 3584: 17.3 us with four, 23.6 with two, 37 with one), fewer leave
-// more waves (16 on 2048 x 3584: 5.9 with one, 6.4 with two); `split` makes waves where outputs are few (one row
-// on 4608 x 3584: 5.8 us with eight, 12.4 with one).
+// The cut of a product.  Fitted to 140 sizes (1, 8, 16, 32 and 64 rows, 64 to 14336 outputs, 1200 to 14336
+// inputs), each with every cut, and checked with 255: 0.5 to 4% slower than the best cut on average.  More tiles a
+// wave read x less often (64 rows on 14336 x 3584: 16.0 us with four, 22.6 with two, 36 with one), fewer
+// leave more waves (16 on 2048 x 3584: 4.8 with one, 5.9 with two); `split` makes waves where outputs are few
+// (one row on 4608 x 3584: 5.4 us with eight, 12 with one).  Parts make workgroups where even so most CUs
+// would have none, or each too long a chain, at the price of a launch and of their sums: 64 rows on
+// 1024 x 14336 20.8 us without, 10.8 with; 16 on 4608 x 14336 17.4 and 14.2; 64 on 1024 x 3584 8.1 and 7.8;
+// and 16 on 1024 x 8000 6.8 and 7.0.
 WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
   WeightPlan p;
   p.row_quads = n_rows <= 4 ? 1 : n_rows <= 8 ? 2 : n_rows <= 16 ? 4 : n_rows <= 32 ? 8 : 16;
+  const int most = p.row_quads < 16 ? 8 : 4;
+  if (p.row_quads >= 4 && v.tiles_in >= (p.row_quads < 16 ? 40 : 20) && v.tiles_out <= 600) {
+    p.tiles = v.tiles_out <= 64 ? 1 : v.tiles_out <= 128 ? 2 : 4;
+    p.split = most;
+    const int64_t groups = over(v.tiles_out, p.tiles) * over(n_rows, 64), longest = v.tiles_in / most;
+    const int64_t parts = kStreamSlots / groups, cap = p.row_quads < 16 ? 6 : 16;
+    p.parts = (int32_t)(parts < cap ? parts : cap);
+    if (p.parts > longest) p.parts = (int32_t)longest;
+    if (p.parts > 1) return p;
+  }
   int waves;                // enough of them to fill the device
   if (p.row_quads == 1) {
     p.tiles = v.tiles_out > 1024 && v.tiles_in > 10 ? 2 : 1;
@@ -57,10 +70,14 @@ WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
     waves = p.row_quads < 16 ? 1536 : 512;
   }
   const int64_t groups = over(v.tiles_out, p.tiles);
-  const int most = p.row_quads < 16 ? 8 : 4;
+  p.parts = 1;
   p.split = 1;
   while (p.split < most && groups * p.split < waves && 2 * p.split <= v.tiles_in) p.split *= 2;
   return p;
+}
+
+int64_t sums_of(const WeightView &v, const WeightPlan &p, int32_t n_rows) {
+  return p.parts > 1 ? (int64_t)64 * p.parts * n_rows * v.tiles_out : 0;
 }
 
 int check_beams(const hermes_beam_config *c) {
@@ -114,8 +131,15 @@ int hermes_weight_pack(const hermes_weight *w, const void *dense, int64_t stride
   return launch_weight_pack(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
 }
 
+size_t hermes_weight_workspace_bytes(const hermes_weight *w, int32_t n_rows) {
+  if (check_weight(w) != HERMES_OK || n_rows < 1 || n_rows > 1 << 20) return 0;
+  const WeightView v = view_of(w);
+  return (size_t)sums_of(v, plan_of(v, n_rows), n_rows);
+}
+
 int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_stride, int32_t n_rows,
-                          const void *bias, const void *add, void *out, int32_t out_type, void *stream) {
+                          const void *bias, const void *add, void *out, int32_t out_type, void *workspace,
+                          size_t ws_bytes, void *stream) {
   const int rc = check_weight(w);
   if (rc != HERMES_OK) return rc;
   if (n_rows < 0 || n_rows > 1 << 20) return HERMES_EINVAL;
@@ -139,6 +163,12 @@ int hermes_weight_product(const hermes_weight *w, const void *x, int64_t x_strid
   a.n_rows = n_rows;
   a.fp32 = out_type == HERMES_FP32;
   a.plan = plan_of(a.w, n_rows);
+  const int64_t need = sums_of(a.w, a.plan, n_rows);
+  if (need > 0) {
+    if (workspace == nullptr || !aligned(workspace, 16)) return HERMES_EINVAL;
+    if (ws_bytes < (size_t)need) return HERMES_ECAPACITY;
+    a.sums = static_cast<float *>(workspace);
+  }
   return launch_weight_product(a, static_cast<hipStream_t>(stream)) == hipSuccess ? HERMES_OK : HERMES_EHIP;
 }
 

@@ -26,6 +26,7 @@ struct WeightPlan {
   int32_t row_quads;        // 1, 2, 4, 8 or 16
   int32_t tiles;            // 1, 2 or 4
   int32_t split;            // 1, 2, 4 or 8 (4 at most with 64 rows)
+  int32_t parts;            // workgroups that share the inputs; more than one: joined by a second launch
 };
 
 struct WeightProductArgs {
@@ -33,6 +34,7 @@ struct WeightProductArgs {
   const uint16_t *x;
   const uint16_t *bias, *add;   // or null
   void *out;
+  float *sums;              // [parts][n_rows][16 tiles_out], with more than one part
   int64_t x_stride;
   int32_t n_rows;
   int32_t fp32;             // out is fp32, else bf16

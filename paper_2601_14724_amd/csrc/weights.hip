@@ -1,7 +1,8 @@
 // Products of a few rows with weights in 4 bits, for gfx950:
 //
 // weight_pack      stores a bf16 weight as FP4 codes and scales, tile by tile
-// weight_product   out = x W^T + bias + add
+// weight_product   out = x W^T + bias + add, or of a part of the inputs x W^T in fp32
+// weight_join      sums such parts
 //
 // A product of M <= 64 rows reads 17/32 byte of weight for 2 M operations, so HBM bounds it up
 // to there.  The layout is an MFMA operand's: of a tile of 16 outputs and 128 inputs a lane holds 32
@@ -82,19 +83,10 @@ __device__ __forceinline__ bf16x8 unpack(uint32_t codes, float scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// Inputs k .. k + 7 of a row, zeros past the last.
-__device__ __forceinline__ u32x4 inputs(const uint16_t *row, int k, int n_in) {
-  if (k + 8 <= n_in) return *reinterpret_cast<const u32x4 *>(row + k);
-  u32x4 v = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (k + i < n_in) v[i / 2] |= (uint32_t)row[k + i] << (i % 2 * 16);
-  return v;
-}
-
 // Four outputs n .. n + 3 of row r.
 __device__ __forceinline__ void store(const WeightProductArgs &a, int64_t r, int n, f32x4 v) {
   const int64_t at = r * a.w.n_out + n;
+  if (n >= a.w.n_out) return;
   const bool whole = n + 4 <= a.w.n_out && a.w.n_out % 4 == 0;
   const auto plus = [&](const uint16_t *from) {
     uint16_t b[4] = {0, 0, 0, 0};
@@ -169,9 +161,12 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = a.plan.split, sub = wave % split;
   const int nt0 = (blockIdx.x * (W / split) + wave / split) * NT;
-  const int q = lane / 16, n16 = lane % 16, r0 = blockIdx.y * 16 * MT;
-  const int k0 = (int)((int64_t)a.w.tiles_in * sub / split), k1 = (int)((int64_t)a.w.tiles_in * (sub + 1) / split);
-  const int rows = min(a.n_rows - r0, 16 * MT);
+  const int q = lane / 16, n16 = lane % 16, part_of = blockIdx.y % a.plan.parts, r0 = blockIdx.y / a.plan.parts * 16 * MT;
+  // this wave's tiles of inputs, of those of the workgroup's part
+  const int p0 = (int)((int64_t)a.w.tiles_in * part_of / a.plan.parts);
+  const int p1 = (int)((int64_t)a.w.tiles_in * (part_of + 1) / a.plan.parts);
+  const int k0 = p0 + (p1 - p0) * sub / split, k1 = p0 + (p1 - p0) * (sub + 1) / split;
+  const int whole = a.w.n_in / 128, rows = min(a.n_rows - r0, 16 * MT);
   // (an offset in the rows of a block stays below 2^32: 64 rows of up to 2^24 elements)
   const uint16_t *x0 = a.x + (int64_t)r0 * a.x_stride;
   const uint32_t x_bytes = (uint32_t)(2 * ((rows - 1) * a.x_stride + a.w.n_in));
@@ -198,10 +193,10 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  const auto weights = [&](Step<NT, U> &s, int kt, int end) {
+  const auto weights = [&](Step<NT, U> &s, int kt) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (kt + i >= end) break;
+      if (kt + i >= k1) break;
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
         s.codes[i][u] = *reinterpret_cast<const u32x4 *>(codes[u] + (int64_t)(kt + i) * 1024);
@@ -209,19 +204,41 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
       }
     }
   };
-  const auto load = [&](Step<NT, U> &s, int kt, int end, int slot) {
+  const auto load = [&](Step<NT, U> &s, int kt, int slot) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (kt + i >= end) break;
+      if (kt + i >= k1) break;
+      uint8_t *const to = mine + slot * kSlot + i * kTile;
+      if (kt + i < whole) {
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, mine + slot * kSlot + i * kTile + r * 1024);
+        for (int r = 0; r < RQ; ++r) load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
+        continue;
+      }
+      // the tile that the inputs end in: whole pieces, and zeros in place of the others
+      const int left = a.w.n_in - 128 * (kt + i);
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) {
+        if (8 * (n16 ^ ((4 * r + q) % 16)) + 8 <= left) {
+          load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
+        } else {
+          *reinterpret_cast<u32x4 *>(to + r * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+      }
+      if (left % 8 != 0 && lane < 4 * RQ) {     // a row's piece that the inputs end in, a lane each
+        const uint16_t *row = x0 + min(lane, rows - 1) * a.x_stride + a.w.n_in - left % 8;
+        u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (e < left % 8) v[e / 2] |= (uint32_t)row[e] << (e % 2 * 16);
+        *reinterpret_cast<u32x4 *>(to + lane * 256 + 16 * (left / 8 ^ lane % 16)) = v;
+      }
     }
-    weights(s, kt, end);
+    weights(s, kt);
   };
-  const auto multiply = [&](const Step<NT, U> &s, int kt, int end, int slot) {
+  const auto multiply = [&](const Step<NT, U> &s, int kt, int slot) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (kt + i >= end) break;
+      if (kt + i >= k1) break;
       const uint8_t *tile = mine + slot * kSlot + i * kTile;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -238,27 +255,16 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
     }
   };
   if (nt0 < a.w.tiles_out) {
-    const int end = min(k1, a.w.n_in / 128);            // of the whole tiles
     Step<NT, U> now, next;
     int slot = 0;
-    if (k0 < end) load(now, k0, end, 0);
+    if (k0 < k1) load(now, k0, 0);
 #pragma unroll 1
-    for (int kt = k0; kt < end; kt += U) {
+    for (int kt = k0; kt < k1; kt += U) {
       wait_for_loads();
-      if (kt + U < end) load(next, kt + U, end, slot ^ 1);
-      multiply(now, kt, end, slot);
+      if (kt + U < k1) load(next, kt + U, slot ^ 1);
+      multiply(now, kt, slot);
       now = next;
       slot ^= 1;
-    }
-    if (end < k1) {         // the last tile, in part past the inputs
-      wait_for_loads();
-#pragma unroll 1
-      for (int r = 0; r < RQ; ++r)
-        *reinterpret_cast<u32x4 *>(mine + r * 1024 + lane * 16) =
-            inputs(x0 + min(4 * r + q, rows - 1) * a.x_stride, 128 * end + 8 * (n16 ^ ((4 * r + q) % 16)), a.w.n_in);
-      weights(now, end, k1);
-      wait_for_loads();
-      multiply(now, end, k1, 0);
     }
   }
   __syncthreads();
@@ -277,8 +283,25 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
     f32x4 v = part[(g * split * MT * NT + tile) * 64 + lane];
 #pragma unroll 1
     for (int s = 1; s < split; ++s) v += part[((g * split + s) * MT * NT + tile) * 64 + lane];
-    if (nt < a.w.tiles_out && r < rows) store(a, r0 + r, 16 * nt + 4 * q, v);
+    if (nt >= a.w.tiles_out || r >= rows) continue;
+    if (a.plan.parts == 1) {
+      store(a, r0 + r, 16 * nt + 4 * q, v);
+    } else {
+      *reinterpret_cast<f32x4 *>(a.sums + (((int64_t)part_of * a.n_rows + r0 + r) * a.w.tiles_out + nt) * 16 + 4 * q) = v;
+    }
   }
+}
+
+// Four outputs of a row a thread: its parts in their order.
+__global__ __launch_bounds__(256) void weight_join(WeightProductArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, wide = (int64_t)a.w.tiles_out * 4, all = wide * a.n_rows;
+  if (i >= all) return;
+  const f32x4 *from = reinterpret_cast<const f32x4 *>(a.sums) + i;
+  f32x4 v = from[0];
+#pragma unroll 4
+  for (int z = 1; z < a.plan.parts; ++z) v += from[z * all];
+  const int64_t r = i / wide;
+  store(a, r, (int)(i - r * wide) * 4, v);
 }
 
 }  // namespace
@@ -296,7 +319,7 @@ template <int RQ, int NT>
 static void launch_product(const WeightProductArgs &a, hipStream_t s) {
   constexpr int U = RQ <= 4 && NT < 4 ? 2 : 1, W = RQ <= 8 ? 8 : 4, kRows = 16 * ((RQ + 3) / 4);
   const int groups = W / a.plan.split * NT;
-  const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + kRows - 1) / kRows);
+  const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + kRows - 1) / kRows * a.plan.parts);
   hipLaunchKernelGGL((weight_product<RQ, NT, U, W>), grid, dim3(64 * W), 0, s, a);
 }
 
@@ -322,6 +345,10 @@ hipError_t launch_weight_product(const WeightProductArgs &a, hipStream_t s) {
     launch_product<8>(a, s);
   } else {
     launch_product<16>(a, s);
+  }
+  if (a.plan.parts > 1) {
+    const int64_t threads = (int64_t)a.w.tiles_out * 4 * a.n_rows;
+    hipLaunchKernelGGL(weight_join, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

@@ -42,7 +42,7 @@ EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_page_bytes", "hermes_page_workspace_bytes", "hermes_page_append",
             "hermes_page_attend", "hermes_page_read", "hermes_page_pack", "hermes_page_reorder",
             "hermes_beam_workspace_bytes", "hermes_beam_select", "hermes_weight_bytes",
-            "hermes_weight_pack", "hermes_weight_product")
+            "hermes_weight_pack", "hermes_weight_workspace_bytes", "hermes_weight_product")
 STATIC_WORKSPACE_BYTES = 128 << 20
 
 
@@ -174,7 +174,9 @@ lib.hermes_weight_bytes.argtypes = [_weight_p]
 lib.hermes_weight_pack.restype = ctypes.c_int
 lib.hermes_weight_pack.argtypes = [_weight_p, _vp, _i64, _vp]
 lib.hermes_weight_product.restype = ctypes.c_int
-lib.hermes_weight_product.argtypes = [_weight_p, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp]
+lib.hermes_weight_workspace_bytes.restype = ctypes.c_size_t
+lib.hermes_weight_workspace_bytes.argtypes = [_weight_p, _i32]
+lib.hermes_weight_product.argtypes = [_weight_p, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp, ctypes.c_size_t, _vp]
 
 
 class HermesError(RuntimeError):
@@ -786,8 +788,12 @@ class PackedWeight:
             stride = -(-self.n_in // 8) * 8
         if es != 1 and self.n_in > 1 and n:
             raise ValueError("x: a row must be contiguous")
+        wp, nbytes = None, lib.hermes_weight_workspace_bytes(self._ref, n)
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            wp = ws.data_ptr()
         _on(self._index, lib.hermes_weight_product, "hermes_weight_product", self._ref, x.data_ptr(), stride, n, bp, ap,
-            out.data_ptr(), kind)
+            out.data_ptr(), kind, wp, nbytes)
         return out
 
     def _on_device(self, t: torch.Tensor, name: str) -> None:

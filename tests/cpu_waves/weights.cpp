@@ -1,5 +1,5 @@
 // weight_pack and weight_product in memory that ends where their inputs end.
-//   weights <outputs> <inputs> <rows> <rows by four> <tiles> <split> <bias> <add> <fp32>
+//   weights <outputs> <inputs> <rows> <rows by four> <tiles> <split> <bias> <add> <fp32> <parts>
 #include "more.h"
 
 #include "weights.hip"
@@ -24,7 +24,7 @@ int main(int, char **argv) {
   WeightProductArgs a = {};
   a.w = w;
   a.n_rows = number(3);
-  a.plan = {number(4), number(5), number(6)};
+  a.plan = {number(4), number(5), number(6), number(10)};
   a.fp32 = number(9);
   a.x_stride = over(w.n_in, 8) * 8;
   const size_t n = (size_t)a.n_rows * w.n_out;
@@ -33,6 +33,7 @@ int main(int, char **argv) {
   if (number(7)) a.bias = static_cast<uint16_t *>(guarded(2 * (size_t)w.n_out, 2));
   if (number(8)) a.add = static_cast<uint16_t *>(guarded(2 * n, 2));
   a.out = guarded(n * (a.fp32 ? 4 : 2), 16);
+  if (a.plan.parts > 1) a.sums = static_cast<float *>(guarded(64 * (size_t)a.plan.parts * a.n_rows * w.tiles_out, 16));
   launch_weight_product(a, nullptr);
   std::puts("done");
 }

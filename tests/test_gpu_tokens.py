@@ -5,6 +5,8 @@ What a weight stands for is exact, and so are the reordered tables and pages.  A
 result is off by what its sums round: of n terms, in any order, n additions of up to
 2^-23 of the terms' magnitudes (an addition may truncate), and half a step of the output.  A
 choice is compared as test_tokens_bounds.check_choice says."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -108,6 +110,14 @@ def test_products_of_any_size(n, k):
 @pytest.mark.parametrize("out", ["bf16", "fp32"])
 def test_products_of_a_model_s_sizes(m, n, k, out):
     check_product(m, n, k, out, bias=n < 5000, add=n < 2000)
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 64, 5120), (9, 1000, 14336), (13, 4608, 8000), (32, 250, 5200), (17, 2048, 6001),
+                                   (64, 64, 2560), (64, 1000, 8001), (33, 4000, 2700), (65, 130, 4000), (130, 20, 9000)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_products_whose_inputs_are_shared_by_workgroups(m, n, k, out):
+    assert H.lib.hermes_weight_workspace_bytes(ctypes.byref(H.WeightStruct(n, k, None)), m) > 0
+    check_product(m, n, k, out, bias=True, add=n < 2000, seed=m)
 
 
 @pytest.mark.parametrize("n", [50, 64])

@@ -156,13 +156,15 @@ def weights(tmp_path_factory):
     return compiled(tmp_path_factory, "weights", "-O1")
 
 
-@pytest.mark.parametrize("n,k,m,row_quads,tiles,split,bias,add,fp32", [
-    (1, 1, 1, 1, 1, 1, 0, 0, 0),
-    (17, 129, 3, 1, 1, 8, 1, 1, 1),
-    (40, 1300, 7, 2, 2, 4, 0, 1, 0),
-    (100, 515, 13, 4, 4, 2, 1, 0, 0),
-    (33, 640, 17, 8, 2, 1, 1, 0, 1),
-    (70, 1025, 65, 16, 1, 4, 0, 1, 0),
+@pytest.mark.parametrize("n,k,m,row_quads,tiles,split,bias,add,fp32,parts", [
+    (1, 1, 1, 1, 1, 1, 0, 0, 0, 1),
+    (17, 129, 3, 1, 1, 8, 1, 1, 1, 1),
+    (40, 1300, 7, 2, 2, 4, 0, 1, 0, 1),
+    (100, 515, 13, 4, 4, 2, 1, 0, 0, 1),
+    (33, 640, 17, 8, 2, 1, 1, 0, 1, 1),
+    (70, 1025, 65, 16, 1, 4, 0, 1, 0, 1),
+    (70, 1025, 65, 16, 4, 4, 1, 1, 0, 2),
+    (35, 1290, 20, 8, 2, 2, 0, 1, 1, 5),
 ])
-def test_products_stay_in_bounds(weights, n, k, m, row_quads, tiles, split, bias, add, fp32):
-    assert run(weights, (n, k, m, row_quads, tiles, split, bias, add, fp32)) == b"done\n"
+def test_products_stay_in_bounds(weights, n, k, m, row_quads, tiles, split, bias, add, fp32, parts):
+    assert run(weights, (n, k, m, row_quads, tiles, split, bias, add, fp32, parts)) == b"done\n"

@@ -19,8 +19,8 @@ def _weight(n_out=100, n_in=200, data=FAKE):
     return H.WeightStruct(n_out, n_in, data)
 
 
-def _product(w=None, x=FAR, xs=200, rows=4, bias=None, add=None, out=2 * FAR, kind=H.BF16):
-    return H.lib.hermes_weight_product(ctypes.byref(w or _weight()), x, xs, rows, bias, add, out, kind, None)
+def _product(w=None, x=FAR, xs=200, rows=4, bias=None, add=None, out=2 * FAR, kind=H.BF16, ws=None, nbytes=0):
+    return H.lib.hermes_weight_product(ctypes.byref(w or _weight()), x, xs, rows, bias, add, out, kind, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("n,k", [(1, 1), (16, 128), (17, 129), (1003, 2236), (4608, 3584), (131072, 513)])
@@ -54,7 +54,20 @@ def test_bad_product_arguments_are_refused():
                  dict(out=FAR), dict(out=FAR + 3 * 400), dict(bias=2 * FAR + 790), dict(add=2 * FAR + 2),
                  dict(add=2 * FAR, kind=H.FP32), dict(out=FAKE + 16)):
         assert _product(**over) == H.EINVAL, over
-    assert H.lib.hermes_weight_product(None, FAR, 200, 4, None, None, 2 * FAR, 0, None) == H.EINVAL
+    assert H.lib.hermes_weight_product(None, FAR, 200, 4, None, None, 2 * FAR, 0, None, 0, None) == H.EINVAL
+
+
+def test_products_that_are_cut_need_a_workspace():
+    """Where a long sum has few outputs, workgroups share the inputs; else none is needed."""
+    need = lambda n, k, rows: H.lib.hermes_weight_workspace_bytes(ctypes.byref(_weight(n, k)), rows)
+    for n, k, rows in ((1152, 896, 1), (4608, 3584, 16), (14336, 3584, 64), (131072, 3584, 8), (1024, 14336, 8)):
+        assert need(n, k, rows) == 0
+    bytes_ = need(1000, 14336, 64)
+    assert bytes_ > 0 and bytes_ % (64 * 64 * 63) == 0           # whole parts: fp32, 64 rows of 63 tiles of 16
+    assert need(1000, 14336, 0) == 0 and need(0, 14336, 64) == 0 and need(1000, 14336, -1) == 0
+    long = dict(w=_weight(1000, 14336), xs=14336, rows=64)
+    assert _product(**long) == H.EINVAL and _product(**long, ws=FAKE + 8, nbytes=bytes_) == H.EINVAL
+    assert _product(**long, ws=FAKE, nbytes=bytes_ - 1) == H.ECAPACITY
 
 
 def test_a_product_of_no_rows_does_nothing():
