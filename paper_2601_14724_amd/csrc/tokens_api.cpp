@@ -51,11 +51,11 @@ int64_t bytes_of(const WeightView &v) {
 WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
   WeightPlan p;
   p.row_quads = n_rows <= 4 ? 1 : n_rows <= 8 ? 2 : n_rows <= 16 ? 4 : n_rows <= 32 ? 8 : 16;
-  const int most = p.row_quads < 16 ? 8 : 4;
+  const int most = p.row_quads < 16 ? 3 : 2;    // waves that share inputs, their log
   if (p.row_quads >= 4 && v.tiles_in >= (p.row_quads < 16 ? 40 : 20) && v.tiles_out <= 600) {
     p.tiles = v.tiles_out <= 64 ? 1 : v.tiles_out <= 128 ? 2 : 4;
-    p.split = most;
-    const int64_t groups = over(v.tiles_out, p.tiles) * over(n_rows, 64), longest = v.tiles_in / most;
+    p.log_split = most;
+    const int64_t groups = over(v.tiles_out, p.tiles) * over(n_rows, 64), longest = v.tiles_in >> most;
     const int64_t parts = kStreamSlots / groups, cap = p.row_quads < 16 ? 6 : 16;
     p.parts = (int32_t)(parts < cap ? parts : cap);
     if (p.parts > longest) p.parts = (int32_t)longest;
@@ -71,8 +71,8 @@ WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
   }
   const int64_t groups = over(v.tiles_out, p.tiles);
   p.parts = 1;
-  p.split = 1;
-  while (p.split < most && groups * p.split < waves && 2 * p.split <= v.tiles_in) p.split *= 2;
+  p.log_split = 0;
+  while (p.log_split < most && groups << p.log_split < waves && 2 << p.log_split <= v.tiles_in) ++p.log_split;
   return p;
 }
 

@@ -25,7 +25,7 @@ struct WeightPackArgs {
 struct WeightPlan {
   int32_t row_quads;        // 1, 2, 4, 8 or 16
   int32_t tiles;            // 1, 2 or 4
-  int32_t split;            // 1, 2, 4 or 8 (4 at most with 64 rows)
+  int32_t log_split;        // split: 1, 2, 4 or 8 (4 at most with 64 rows)
   int32_t parts;            // workgroups that share the inputs; more than one: joined by a second launch
 };
 

@@ -159,13 +159,18 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   constexpr int kRoom = 2 * kSlot * W > W * MT * NT * 1024 ? 2 * kSlot * W : W * MT * NT * 1024;
   __shared__ __attribute__((aligned(16))) uint8_t room[kRoom];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = a.plan.split, sub = wave % split;
-  const int nt0 = (blockIdx.x * (W / split) + wave / split) * NT;
-  const int q = lane / 16, n16 = lane % 16, part_of = blockIdx.y % a.plan.parts, r0 = blockIdx.y / a.plan.parts * 16 * MT;
+  const int split = 1 << a.plan.log_split, groups = W >> a.plan.log_split, sub = wave & (split - 1);
+  const int nt0 = ((int)blockIdx.x * groups + (wave >> a.plan.log_split)) * NT;
+  const int q = lane / 16, n16 = lane % 16;
   // this wave's tiles of inputs, of those of the workgroup's part
-  const int p0 = (int)((int64_t)a.w.tiles_in * part_of / a.plan.parts);
-  const int p1 = (int)((int64_t)a.w.tiles_in * (part_of + 1) / a.plan.parts);
-  const int k0 = p0 + (p1 - p0) * sub / split, k1 = p0 + (p1 - p0) * (sub + 1) / split;
+  int r0 = (int)blockIdx.y * 16 * MT, z = 0, p0 = 0, p1 = a.w.tiles_in;
+  if (a.plan.parts > 1) {
+    z = blockIdx.y % a.plan.parts;
+    r0 = blockIdx.y / a.plan.parts * 16 * MT;
+    p0 = a.w.tiles_in * z / a.plan.parts;
+    p1 = a.w.tiles_in * (z + 1) / a.plan.parts;
+  }
+  const int k0 = p0 + ((p1 - p0) * sub >> a.plan.log_split), k1 = p0 + ((p1 - p0) * (sub + 1) >> a.plan.log_split);
   const int whole = a.w.n_in / 128, rows = min(a.n_rows - r0, 16 * MT);
   // (an offset in the rows of a block stays below 2^32: 64 rows of up to 2^24 elements)
   const uint16_t *x0 = a.x + (int64_t)r0 * a.x_stride;
@@ -275,7 +280,6 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
     for (int t = 0; t < MT; ++t) part[(wave * MT * NT + u * MT + t) * 64 + lane] = acc[u][t];
   __syncthreads();
   // tile i of group g: summed over the group's waves, in their order
-  const int groups = W / split;
 #pragma unroll 1
   for (int i = wave; i < groups * NT * MT; i += W) {
     const int g = i / (NT * MT), tile = i % (NT * MT);
@@ -287,7 +291,7 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
     if (a.plan.parts == 1) {
       store(a, r0 + r, 16 * nt + 4 * q, v);
     } else {
-      *reinterpret_cast<f32x4 *>(a.sums + (((int64_t)part_of * a.n_rows + r0 + r) * a.w.tiles_out + nt) * 16 + 4 * q) = v;
+      *reinterpret_cast<f32x4 *>(a.sums + (((int64_t)z * a.n_rows + r0 + r) * a.w.tiles_out + nt) * 16 + 4 * q) = v;
     }
   }
 }
@@ -318,7 +322,7 @@ hipError_t launch_weight_pack(const WeightPackArgs &a, hipStream_t s) {
 template <int RQ, int NT>
 static void launch_product(const WeightProductArgs &a, hipStream_t s) {
   constexpr int U = RQ <= 4 && NT < 4 ? 2 : 1, W = RQ <= 8 ? 8 : 4, kRows = 16 * ((RQ + 3) / 4);
-  const int groups = W / a.plan.split * NT;
+  const int groups = (W >> a.plan.log_split) * NT;
   const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + kRows - 1) / kRows * a.plan.parts);
   hipLaunchKernelGGL((weight_product<RQ, NT, U, W>), grid, dim3(64 * W), 0, s, a);
 }
