@@ -18,9 +18,9 @@
 // Term by term that is 1e-6 at worst (an argument of 16 octaves and more has half an ulp of 2^-20), which
 // logits that differ average out: 1e-8.
 //
-// Measured: 16 sequences of eight beams over 131072 tokens in bf16, 34 MB, 9.7 us (85 vector instructions
-// for 512 logits a wave, the exponentials four of them each: as much as HBM's rate allows) and 9.7 for the choice;
-// 32 of 16 in fp32, 268 MB, 44 us (6.1 TB/s; part of it stays in the Infinity Cache) and 12.8.  The choice is a
+// Measured: 16 sequences of eight beams over 131072 tokens in bf16, 34 MB, 9.7 us (88 vector instructions
+// for 512 logits, its eight exponentials four issue slots each) and 9.5 for the choice; 32 of 16 in fp32,
+// 268 MB, 45 us (6 TB/s; part of it stays in the Infinity Cache) and 13.6.  The choice is a
 // workgroup a sequence, a chain of loads, moves and barriers: 7.7 us where it is short.  Its code is kept
 // small: it runs once, so that every line is fetched (62 KB of unrolled loops took 8.7 us for 7.3).
 #include "tokens_internal.h"

@@ -10,8 +10,9 @@
 // (v_cvt_scalef32_pk_bf16_fp4, two values an instruction), x is bf16, and
 // v_mfma_f32_16x16x32_bf16 sums in fp32, so what is rounded is the sum alone.
 //
-// Measured (calls in one graph, weights not in the caches): 8 rows of 3584 on 131072 outputs 46.5 us,
-// 5.46 TB/s; one row on 4608 5.8, on 1152 x 896 3.3 (an empty launch: 1.8); 64 rows on 14336 17.3.
+// Measured (calls in one graph, weights not in the caches; an empty launch takes 1.8 us): 8 rows of 3584 on
+// 131072 outputs 46.6 us, 5.4 TB/s; one row on 4608 5.3, on 1152 x 896 2.9; 16 on 4608 6.7; 64 on 14336 15.6,
+// bound by L2, from which each workgroup reads all of x.
 #include "tokens_internal.h"
 
 namespace hermes {
@@ -148,7 +149,7 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, ui
 //
 // x reaches the lanes through LDS, a tile's 128 inputs of a row in 256 bytes, 16 lanes a row: as
 // fragments straight from memory 16 neighbouring lanes' pieces lie in 16 rows, and the loads take longer than
-// the weight's (64 rows on 14336 x 3584 23.8 us so, 17.3 through LDS; 8 rows on 131072 54.9 and 46.0).  Piece c
+// the weight's (64 rows on 14336 x 3584 23.8 us so, 17.3 through LDS; 8 rows on 131072 54.9 and 46.0, both in the first form).  Piece c
 // of row r lies at c ^ (r % 16), so that neither the loads nor the fragments' reads meet in a
 // bank.  LDS is each wave's own (waves that share outputs have different inputs), so there is no
 // barrier before their sums are joined, and while a step is multiplied the next one's loads run.
