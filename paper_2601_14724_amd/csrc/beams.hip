@@ -203,7 +203,7 @@ __device__ __forceinline__ bool before(double v, int i, double w, int j) { retur
 
 constexpr int kList = 2048, kPickWaves = kPickThreads / 64;
 constexpr int kGroup = kPickThreads / 64;   // threads of a group: 64 groups
-static_assert(kGroup == 8 || kGroup == 16, "reduced by three or four moves");
+static_assert(kGroup == 16, "reduced by four moves");
 
 struct PickShared {
   double offset[kMaxBeams];         // score - ln sum exp; a done beam: its score; -infinity: offers nothing
@@ -238,8 +238,7 @@ __device__ __forceinline__ int group_sum(int x) {
   x += moved<kXor1>(x);
   x += moved<kXor2>(x);
   x += moved<kHalfMirror>(x);
-  if constexpr (kGroup == 16) x += moved<kMirror>(x);
-  return x;
+  return x + moved<kMirror>(x);
 }
 
 // Orders as the value does (-0 and 0 alike).

@@ -149,8 +149,8 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, ui
 //
 // x reaches the lanes through LDS, a tile's 128 inputs of a row in 256 bytes, 16 lanes a row: as
 // fragments straight from memory 16 neighbouring lanes' pieces lie in 16 rows, and the loads take longer than
-// the weight's (64 rows on 14336 x 3584 23.8 us so, 17.3 through LDS; 8 rows on 131072 54.9 and 46.0, both in the first form).  Piece c
-// of row r lies at c ^ (r % 16), so that neither the loads nor the fragments' reads meet in a
+// the weight's (64 rows on 14336 x 3584 23.8 us so, 17.3 through LDS; 8 rows on 131072 54.9 and 46.0, before
+// the steps since).  Piece c of row r lies at c ^ (r % 16), so that neither the loads nor the fragments' reads meet in a
 // bank.  LDS is each wave's own (waves that share outputs have different inputs), so there is no
 // barrier before their sums are joined, and while a step is multiplied the next one's loads run.
 template <int RQ, int NT, int U, int W>

@@ -758,9 +758,9 @@ class PackedWeight:
 
     def product(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-        """x [n_rows][n_in] (bf16, rows may lie apart) times the weight's transpose, plus bias [n_out]
-        and add [n_rows][n_out] (bf16): [n_rows][n_out] of bf16 or fp32 (`dtype`, or `out`'s).
-        out may be add."""
+        """x [n_rows][n_in] (bf16, 16-byte aligned, rows a multiple of 8 elements apart) times the weight's
+        transpose, plus bias [n_out] and add [n_rows][n_out] (bf16): [n_rows][n_out] of bf16 or fp32
+        (`dtype`, or `out`'s).  out may be add."""
         if not isinstance(x, torch.Tensor) or x.dtype is not torch.bfloat16 or x.dim() != 2 or x.shape[1] != self.n_in:
             raise ValueError(f"x: expected torch.bfloat16 [n_rows][{self.n_in}], got {getattr(x, 'dtype', None)} "
                              f"{tuple(getattr(x, 'shape', ()))}")
@@ -786,8 +786,8 @@ class PackedWeight:
         stride, es = x.stride()
         if n <= 1:
             stride = -(-self.n_in // 8) * 8
-        if es != 1 and self.n_in > 1 and n:
-            raise ValueError("x: a row must be contiguous")
+        if n and (es != 1 and self.n_in > 1 or stride % 8 != 0):
+            raise ValueError("x: a row must be contiguous, and rows a multiple of 8 elements apart")
         wp, nbytes = None, lib.hermes_weight_workspace_bytes(self._ref, n)
         if nbytes:
             ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)

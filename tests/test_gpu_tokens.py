@@ -131,6 +131,27 @@ def test_products_of_strided_rows_and_of_empty_ones():
     assert w.product(torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)).shape == (0, 20)
 
 
+def test_products_refuse_other_tensors():
+    w = H.PackedWeight(bf16(weight_bits(20, 60, 1)))
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device=DEV)
+    w.product(x[:, :60])
+    w.product(torch.zeros(1, 60, dtype=torch.bfloat16, device=DEV))       # (one row lies nowhere apart)
+    row = torch.zeros(4, 20, dtype=torch.bfloat16, device=DEV)
+    for bad in (x, x[:, :60].contiguous(), x[:, :60].float(), x[:, :60].cpu(), torch.zeros(60, 4, device=DEV).to(x.dtype).T):
+        with pytest.raises(ValueError):
+            w.product(bad)
+    for extra in (dict(bias=row[0].float()), dict(bias=row), dict(add=row[:2]), dict(add=row.T), dict(out=row[:3]), dict(out=row.half()),
+                  dict(dtype=torch.float16), dict(bias=row[0].cpu())):
+        with pytest.raises(ValueError):
+            w.product(x[:, :60], **extra)
+    for bad in (torch.zeros(4, 72, dtype=torch.bfloat16, device=DEV)[:, 4:64], x[:1, :60].expand(4, 60)):   # misaligned; one row
+        with pytest.raises(H.HermesError):
+            w.product(bad)
+    room = torch.zeros(400, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(H.HermesError):
+        w.product(room[:256].view(4, 64)[:, :60], out=room[200:280].view(4, 20))
+
+
 def test_a_weight_s_columns_come_back_exactly():
     """x of unit rows: what the weight stands for, bit for bit; and an input's NaN stays in its row."""
     n, k = 70, 300
