@@ -671,11 +671,11 @@ class KVPages:
         self._fits(parent, torch.int32, (n_seqs, n_beams), "parent")
         self._fits(room, torch.int32, shape[:-2] + (2,), "room")
         if tables_out is None:
-            tables_out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            tables_out = torch.empty_like(tables)
         else:
             self._fits(tables_out, torch.int32, shape, "tables_out")
         if kv_len_out is None:
-            kv_len_out = torch.empty(shape[:-1], dtype=torch.int32, device=self.device)
+            kv_len_out = torch.empty_like(kv_len)
         else:
             self._fits(kv_len_out, torch.int32, shape[:-1], "kv_len_out")
         s = PageBeamsStruct(math.prod(shape[:-2]), n_seqs, n_beams, max_pages, grow, parent.data_ptr(), room.data_ptr(),
@@ -717,9 +717,8 @@ def beam_select(logits: torch.Tensor, score: torch.Tensor, keep: int, done: Opti
     ref = ctypes.byref(cfg)
     nbytes = lib.hermes_beam_workspace_bytes(ref)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-    shape = (n_seqs, max(keep, 0))
-    best = torch.empty(shape, dtype=torch.float32, device=logits.device)
-    parent, token, ended = torch.empty((3,) + shape, dtype=torch.int32, device=logits.device).unbind(0)
+    best, parent, token, ended = torch.empty((4, n_seqs, max(keep, 0)), dtype=torch.int32, device=logits.device).unbind(0)
+    best = best.view(torch.float32)
     _on(index, lib.hermes_beam_select, "hermes_beam_select", ref, logits.data_ptr(), stride, score.data_ptr(), _ptr(done),
         best.data_ptr(), parent.data_ptr(), token.data_ptr(), ended.data_ptr(), ws.data_ptr(), nbytes)
     return best, parent, token, ended
