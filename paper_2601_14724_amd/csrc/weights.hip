@@ -153,11 +153,19 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, ui
 // the steps since).  Piece c of row r lies at c ^ (r % 16), so that neither the loads nor the fragments' reads meet in a
 // bank.  LDS is each wave's own (waves that share outputs have different inputs), so there is no
 // barrier before their sums are joined, and while a step is multiplied the next one's loads run.
-template <int RQ, int NT, int U, int W>
+//
+// Common: four waves of the same inputs and of outputs of their own share one x in LDS, a quarter of
+// its rows loaded by each, at a barrier a step; it is read from L2 a quarter as often and nothing is joined.  64 rows
+// of 3584 on 131072 outputs 88 us without and 57 with, of 896 on 40000 16.6 and 12.1; 32 rows of 3584 on 131072 62
+// and 49; 16 rows 51 and 49, on 40000 20.7 and 20.2; up to 8 rows it gains nothing (46.1 and 47.8 on 131072).
+template <int RQ, int NT, int U, int W, bool Common>
 __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   constexpr int MT = (RQ + 3) / 4;                      // tiles of 16 rows
   constexpr int kTile = RQ * 1024, kSlot = U * kTile;   // bytes of x: 4 RQ rows of a tile, of a step
-  constexpr int kRoom = 2 * kSlot * W > W * MT * NT * 1024 ? 2 * kSlot * W : W * MT * NT * 1024;
+  constexpr int kSlots = 2 * kSlot * (Common ? 1 : W), kSums = Common ? 0 : W * MT * NT * 1024;
+  constexpr int kRoom = kSlots > kSums ? kSlots : kSums;
+  constexpr int kMine = Common ? RQ / W : RQ;           // rows that this wave loads, by four
+  static_assert(!Common || RQ % W == 0, "waves load equal shares");
   __shared__ __attribute__((aligned(16))) uint8_t room[kRoom];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = 1 << a.plan.log_split, groups = W >> a.plan.log_split, sub = wave & (split - 1);
@@ -176,13 +184,14 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
   // (an offset in the rows of a block stays below 2^32: 64 rows of up to 2^24 elements)
   const uint16_t *x0 = a.x + (int64_t)r0 * a.x_stride;
   const uint32_t x_bytes = (uint32_t)(2 * ((rows - 1) * a.x_stride + a.w.n_in));
-  uint32_t from[RQ];                    // this lane's piece of row 4 i + q
+  const int quad0 = Common ? wave * kMine : 0;
+  uint32_t from[kMine];                 // this lane's piece of row 4 (quad0 + i) + q
 #pragma unroll
-  for (int i = 0; i < RQ; ++i) {
-    const int r = 4 * i + q;
+  for (int i = 0; i < kMine; ++i) {
+    const int r = 4 * (quad0 + i) + q;
     from[i] = (uint32_t)(min(r, rows - 1) * a.x_stride * 2) + 16 * (n16 ^ (r % 16));
   }
-  uint8_t *const mine = room + wave * 2 * kSlot;
+  uint8_t *const mine = room + (Common ? 0 : wave * 2 * kSlot);
   int at[MT];                           // this lane's row of fragments, and its place in a tile
 #pragma unroll
   for (int t = 0; t < MT; ++t) at[t] = min(16 * t + n16, 4 * RQ - 1);
@@ -217,26 +226,27 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
       uint8_t *const to = mine + slot * kSlot + i * kTile;
       if (kt + i < whole) {
 #pragma unroll
-        for (int r = 0; r < RQ; ++r) load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
+        for (int r = 0; r < kMine; ++r) load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + (quad0 + r) * 1024);
         continue;
       }
       // the tile that the inputs end in: whole pieces, and zeros in place of the others
       const int left = a.w.n_in - 128 * (kt + i);
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) {
-        if (8 * (n16 ^ ((4 * r + q) % 16)) + 8 <= left) {
-          load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + r * 1024);
+      for (int r = 0; r < kMine; ++r) {
+        if (8 * (n16 ^ ((4 * (quad0 + r) + q) % 16)) + 8 <= left) {
+          load_to_lds(x0, x_bytes, from[r], (kt + i) * 256, to + (quad0 + r) * 1024);
         } else {
-          *reinterpret_cast<u32x4 *>(to + r * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4 *>(to + (quad0 + r) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
         }
       }
-      if (left % 8 != 0 && lane < 4 * RQ) {     // a row's piece that the inputs end in, a lane each
-        const uint16_t *row = x0 + min(lane, rows - 1) * a.x_stride + a.w.n_in - left % 8;
+      if (left % 8 != 0 && lane < 4 * kMine) {  // a row's piece that the inputs end in, a lane each
+        const int r = 4 * quad0 + lane;
+        const uint16_t *row = x0 + min(r, rows - 1) * a.x_stride + a.w.n_in - left % 8;
         u32x4 v = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 7; ++e)
           if (e < left % 8) v[e / 2] |= (uint32_t)row[e] << (e % 2 * 16);
-        *reinterpret_cast<u32x4 *>(to + lane * 256 + 16 * (left / 8 ^ lane % 16)) = v;
+        *reinterpret_cast<u32x4 *>(to + r * 256 + 16 * (left / 8 ^ r % 16)) = v;
       }
     }
     weights(s, kt);
@@ -260,18 +270,27 @@ __global__ __launch_bounds__(64 * W) void weight_product(WeightProductArgs a) {
       }
     }
   };
-  if (nt0 < a.w.tiles_out) {
+  if (Common || nt0 < a.w.tiles_out) {
     Step<NT, U> now, next;
     int slot = 0;
     if (k0 < k1) load(now, k0, 0);
 #pragma unroll 1
     for (int kt = k0; kt < k1; kt += U) {
       wait_for_loads();
+      if constexpr (Common) __syncthreads();
       if (kt + U < k1) load(next, kt + U, slot ^ 1);
       multiply(now, kt, slot);
       now = next;
       slot ^= 1;
     }
+  }
+  if constexpr (Common) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+        if (nt0 + u < a.w.tiles_out && 16 * t + n16 < rows) store(a, r0 + 16 * t + n16, 16 * (nt0 + u) + 4 * q, acc[u][t]);
+    return;
   }
   __syncthreads();
   f32x4 *part = reinterpret_cast<f32x4 *>(room);        // [waves][NT MT][64]
@@ -320,12 +339,21 @@ hipError_t launch_weight_pack(const WeightPackArgs &a, hipStream_t s) {
 // Rows by four, tiles of outputs a wave, steps of so many tiles of inputs, waves.  (A workgroup's x
 // is 2 steps x waves x 1 KiB x rows by four: 128 KiB at 16 rows and more, so that workgroups of 64 rows
 // have four waves.)
-template <int RQ, int NT>
+template <int RQ, int NT, int U, int W, bool Common>
 static void launch_product(const WeightProductArgs &a, hipStream_t s) {
-  constexpr int U = RQ <= 4 && NT < 4 ? 2 : 1, W = RQ <= 8 ? 8 : 4, kRows = 16 * ((RQ + 3) / 4);
+  constexpr int kRows = 16 * ((RQ + 3) / 4);
   const int groups = (W >> a.plan.log_split) * NT;
   const dim3 grid((a.w.tiles_out + groups - 1) / groups, (a.n_rows + kRows - 1) / kRows * a.plan.parts);
-  hipLaunchKernelGGL((weight_product<RQ, NT, U, W>), grid, dim3(64 * W), 0, s, a);
+  hipLaunchKernelGGL((weight_product<RQ, NT, U, W, Common>), grid, dim3(64 * W), 0, s, a);
+}
+
+template <int RQ, int NT>
+static void launch_product(const WeightProductArgs &a, hipStream_t s) {
+  if constexpr (RQ >= 4) {
+    // (two steps take 64 KiB at most: two workgroups on a CU)
+    if (a.plan.common) return launch_product<RQ, NT, RQ == 16 ? (NT == 1 ? 2 : 1) : 4 / NT, 4, true>(a, s);
+  }
+  launch_product<RQ, NT, RQ <= 4 && NT < 4 ? 2 : 1, RQ <= 8 ? 8 : 4, false>(a, s);
 }
 
 template <int RQ>

@@ -1,5 +1,5 @@
 // weight_pack and weight_product in memory that ends where their inputs end.
-//   weights <outputs> <inputs> <rows> <rows by four> <tiles> <split> <bias> <add> <fp32> <parts>
+//   weights <outputs> <inputs> <rows> <rows by four> <tiles> <split> <bias> <add> <fp32> <parts> <common>
 #include "more.h"
 
 #include "weights.hip"
@@ -24,7 +24,7 @@ int main(int, char **argv) {
   WeightProductArgs a = {};
   a.w = w;
   a.n_rows = number(3);
-  a.plan = {number(4), number(5), __builtin_ctz(number(6)), number(10)};
+  a.plan = {number(4), number(5), __builtin_ctz(number(6)), number(10), number(11)};
   a.fp32 = number(9);
   a.x_stride = over(w.n_in, 8) * 8;
   const size_t n = (size_t)a.n_rows * w.n_out;

@@ -120,6 +120,14 @@ def test_products_whose_inputs_are_shared_by_workgroups(m, n, k, out):
     check_product(m, n, k, out, bias=True, add=n < 2000, seed=m)
 
 
+@pytest.mark.parametrize("m,n,k", [(9, 16390, 200), (16, 33000, 130), (13, 66001, 64), (17, 16500, 1153), (32, 32800, 40),
+                                   (30, 65600, 129), (33, 17000, 515), (64, 40001, 250), (48, 65540, 127), (100, 9001, 700),
+                                   (200, 4610, 385), (16, 1000, 384), (64, 129, 257), (130, 65, 300), (24, 9000, 1531), (64, 1, 1)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_products_whose_rows_are_shared_by_waves(m, n, k, out):
+    check_product(m, n, k, out, bias=True, add=n < 10000, seed=n)
+
+
 @pytest.mark.parametrize("n", [50, 64])
 def test_a_residual_is_added_in_place(n):
     check_product(9, n, 200, "bf16", bias=True, add=True, stride=264, in_place=True)

@@ -156,6 +156,22 @@ def weights(tmp_path_factory):
     return compiled(tmp_path_factory, "weights", "-O1")
 
 
+@pytest.mark.parametrize("n,k,m,row_quads,tiles,bias,add,fp32", [
+    (1, 1, 9, 4, 1, 0, 0, 0),
+    (70, 515, 16, 4, 1, 1, 1, 0),
+    (150, 1290, 13, 4, 2, 0, 1, 1),
+    (257, 256, 12, 4, 4, 0, 0, 0),
+    (65, 1153, 17, 8, 1, 1, 0, 1),
+    (129, 383, 32, 8, 2, 0, 1, 0),
+    (300, 130, 31, 8, 4, 1, 0, 0),
+    (65, 641, 33, 16, 1, 1, 1, 0),
+    (100, 7, 64, 16, 2, 0, 1, 1),
+    (258, 385, 70, 16, 4, 1, 0, 0),
+])
+def test_products_of_shared_rows_stay_in_bounds(weights, n, k, m, row_quads, tiles, bias, add, fp32):
+    assert run(weights, (n, k, m, row_quads, tiles, 1, bias, add, fp32, 1, 1)) == b"done\n"
+
+
 @pytest.mark.parametrize("n,k,m,row_quads,tiles,split,bias,add,fp32,parts", [
     (1, 1, 1, 1, 1, 1, 0, 0, 0, 1),
     (17, 129, 3, 1, 1, 8, 1, 1, 1, 1),
@@ -167,4 +183,4 @@ def weights(tmp_path_factory):
     (35, 1290, 20, 8, 2, 2, 0, 1, 1, 5),
 ])
 def test_products_stay_in_bounds(weights, n, k, m, row_quads, tiles, split, bias, add, fp32, parts):
-    assert run(weights, (n, k, m, row_quads, tiles, split, bias, add, fp32, parts)) == b"done\n"
+    assert run(weights, (n, k, m, row_quads, tiles, split, bias, add, fp32, parts, 0)) == b"done\n"
