@@ -50,13 +50,14 @@ int64_t bytes_of(const WeightView &v) {
 // and 16 on 1024 x 8000 6.8 and 7.0.
 // Where outputs are many, or inputs few, waves share x (`common`): 64 rows on 14336 x 3584 15.8 us without and
 // 18.6 with, on 18000 x 3584 24.9 and 23.8, on 131072 x 3584 87 and 58; 16 rows on 2048 x 384 3.1 and 2.8, on
-// 2048 x 512 3.1 and 3.3, on 9000 x 1200 5.4 and 5.1, on 9000 x 2236 7.9 and 8.3.  A wave has the fewest tiles that
+// 2048 x 512 3.1 and 3.3, on 9000 x 1200 5.4 and 5.1, on 9000 x 2236 7.9 and 8.3; few inputs of 5 to 8 rows go as
+// 16 do (8 on 131072 x 250 9.7 and 7.6, on 2048 x 384 2.9 and 2.8), of up to 4 not (131072 x 128 4.9 and 5.4).  A wave has the fewest tiles that
 // leave two workgroups a CU at most (64 rows on 24000 x 896: one tile 9.1, two 10.3, four more than 11.3; on
 // 131072 x 3584 two 73, four 58): 3 to 6% slower than the best cut of 111 sizes with 16, 32 and 64 rows,
 // 14336 to 131072 outputs and 896 to 8000 inputs.
 WeightPlan plan_of(const WeightView &v, int32_t n_rows) {
   WeightPlan p;
-  p.row_quads = n_rows <= 4 ? 1 : n_rows <= 8 ? 2 : n_rows <= 16 ? 4 : n_rows <= 32 ? 8 : 16;
+  p.row_quads = n_rows <= 4 ? 1 : n_rows <= 8 && v.tiles_in > 3 ? 2 : n_rows <= 16 ? 4 : n_rows <= 32 ? 8 : 16;
   p.common = 0;
   const int most = p.row_quads < 16 ? 3 : 2;    // waves that share inputs, their log
   if (p.row_quads >= 4 && v.tiles_in >= (p.row_quads < 16 ? 40 : 20) && v.tiles_out <= 600) {

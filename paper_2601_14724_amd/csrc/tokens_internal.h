@@ -27,7 +27,7 @@ struct WeightPlan {
   int32_t tiles;            // 1, 2 or 4
   int32_t log_split;        // split: 1, 2, 4 or 8 (4 at most with 64 rows)
   int32_t parts;            // workgroups that share the inputs; more than one: joined by a second launch
-  int32_t common;           // four waves that share x in LDS (9 rows and more, split and parts 1)
+  int32_t common;           // four waves that share x in LDS (row_quads 4 and more, split and parts 1)
 };
 
 struct WeightProductArgs {

@@ -122,7 +122,8 @@ def test_products_whose_inputs_are_shared_by_workgroups(m, n, k, out):
 
 @pytest.mark.parametrize("m,n,k", [(9, 16390, 200), (16, 33000, 130), (13, 66001, 64), (17, 16500, 1153), (32, 32800, 40),
                                    (30, 65600, 129), (33, 17000, 515), (64, 40001, 250), (48, 65540, 127), (100, 9001, 700),
-                                   (200, 4610, 385), (16, 1000, 384), (64, 129, 257), (130, 65, 300), (24, 9000, 1531), (64, 1, 1)])
+                                   (200, 4610, 385), (16, 1000, 384), (64, 129, 257), (130, 65, 300), (24, 9000, 1531), (64, 1, 1), (5, 20010, 384),
+                                   (8, 40, 129)])
 @pytest.mark.parametrize("out", ["bf16", "fp32"])
 def test_products_whose_rows_are_shared_by_waves(m, n, k, out):
     check_product(m, n, k, out, bias=True, add=n < 10000, seed=n)
