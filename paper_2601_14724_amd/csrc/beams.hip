@@ -309,13 +309,27 @@ __device__ __forceinline__ Candidate bound_of(PickShared &s, int keep, const Set
   return Candidate{s.edge_value, s.edge_index};
 }
 
+// The `keep` first of the `count` in the list, in order, to s.out_value and s.out_index.
+__device__ __forceinline__ void first_of_list(PickShared &s, int keep, int count) {
+  const int group = threadIdx.x / kGroup, slice = threadIdx.x % kGroup;
+  for (int c0 = 0; c0 < count; c0 += 64) {
+    const int c = min(c0 + group, count - 1);
+    const Candidate x{s.value[c], s.index[c]};
+    int first = 0;
+    for (int o = slice; o < count; o += kGroup) first += before(s.value[o], s.index[o], x.v, x.i);
+    first = group_sum(first);
+    if (slice == 0 && c0 + group < count && first < keep) s.out_value[first] = x.v, s.out_index[first] = x.i;
+  }
+  __syncthreads();
+}
+
 // The `keep` first candidates, in order, to s.out_value and s.out_index; how many there are.  At least
 // `keep` reach the edge (or all do): those that do are listed, and a group of threads each counts the
 // ones before it.  Where they are more than the list holds, the edge is raised to the keep-th
 // candidate itself (rows of ties: some 100 us).  s.count is zero.
 template <typename Set>
 __device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Candidate edge) {
-  const int tid = threadIdx.x, group = tid / kGroup, slice = tid % kGroup;
+  const int tid = threadIdx.x;
   for (int round = 0;; ++round) {
     set.above(edge.v, [&](double v, int i) {
       if (v > kNone && !before(edge.v, edge.i, v, i)) {
@@ -331,15 +345,7 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Can
     __syncthreads();
   }
   const int count = min(s.count, kList);
-  for (int c0 = 0; c0 < count; c0 += 64) {
-    const int c = min(c0 + group, count - 1);
-    const Candidate x{s.value[c], s.index[c]};
-    int first = 0;
-    for (int o = slice; o < count; o += kGroup) first += before(s.value[o], s.index[o], x.v, x.i);
-    first = group_sum(first);
-    if (slice == 0 && c0 + group < count && first < keep) s.out_value[first] = x.v, s.out_index[first] = x.i;
-  }
-  __syncthreads();
+  first_of_list(s, keep, count);
   return min(count, keep);
 }
 
@@ -488,7 +494,26 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   if (tid == 0) s.count = 0;
   __syncthreads();
   const Tokens<FP32> tokens(s, a, row0, n_chunks);
-  if (n_chunks < a.n_keep) edge = bound_of(s, a.n_keep, tokens);
+  if (n_chunks < a.n_keep) {
+    // (all chunks were chosen, and nothing bounds their tokens yet)
+    edge.v = kNone;
+    if (n_chunks * kBeamChunk > kList) {
+      // Of the threads' first tokens the n_keep-th does: n_keep reach it, in as many threads unless some tie, and
+      // a thread has 32.  Without it the edge is searched (32 of 16 x 500 tokens: 727 us, 19.7 with it).
+      const Candidate x = tokens.best();
+      if (x.v > kNone) {
+        const int at = atomicAdd(&s.count, 1);
+        s.value[at] = x.v;
+        s.index[at] = tid;
+      }
+      __syncthreads();
+      const int count = s.count;
+      first_of_list(s, a.n_keep, count);
+      if (count >= a.n_keep) edge.v = s.out_value[a.n_keep - 1];
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+    }
+  }
   const int n = pick(s, a.n_keep, tokens, edge);
   if (tid < a.n_keep) {
     const bool some = tid < n;

@@ -361,6 +361,25 @@ def test_rows_that_lie_gibibytes_apart():
     check_choice(x, np.zeros((2, 2), np.float32), None, 5, -1, 0, got)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("seqs,beams,vocab,keep", [(2, 16, 500, 32), (1, 5, 512, 64), (3, 16, 150, 32), (1, 63, 300, 64), (2, 33, 512, 64),
+                                                   (1, 16, 1000, 64)])
+def test_choices_of_more_than_there_are_chunks(seqs, beams, vocab, keep, kind):
+    rng = np.random.default_rng(beams + vocab)
+    x = logits_of(rng, seqs, beams, vocab, kind)
+    score = -rng.random((seqs, beams)).astype(np.float32)
+    done = (rng.random((seqs, beams)) < 0.3).astype(np.int32)
+    choose(x, score, keep, kind)
+    choose(x, score, keep, kind, done=done, end=2, pad_token=2)
+    x[:, 1:, 4:] = -np.inf                          # most threads have nothing
+    x[:, 0, :vocab // 2] = -np.inf
+    choose(x, score, keep, kind, done=done, end=2, pad_token=2)
+    x[:] = 0                                        # all alike
+    choose(x, np.zeros_like(score), keep, kind)
+    x[:, beams // 2] = np.nan
+    choose(x, np.zeros_like(score), keep, kind)
+
+
 def test_choices_of_few_tokens_leave_no_rest():
     got = choose(np.float32([[[1, 2, 3], [3, 2, 1]]]), np.zeros((1, 2), np.float32), 9, "fp32", end=0)
     assert got[1][0].tolist() == [0, 1, 0, 1, 0, 1, -1, -1, -1] and got[2][0].tolist() == [2, 0, 1, 1, 0, 2, -1, -1, -1]

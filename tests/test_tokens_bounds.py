@@ -130,6 +130,8 @@ def check_choice(logits, score, done, keep, end, pad, got, doubt=DOUBT):
     (2, 3, 513, 7, False, 1, True, 1),
     (1, 2, 1500, 64, True, 3, False, 2),
     (2, 2, 40, 64, True, 0, True, 1),
+    (1, 6, 500, 64, False, 0, True, 1),        # fewer chunks than choices, more tokens than the list holds
+    (2, 16, 260, 32, True, 5, False, 1),
 ])
 def test_beam_select_stays_in_bounds_and_gives_the_definition(beams, seqs, n_beams, vocab, keep, fp32, pad, with_done, per):
     rng = np.random.default_rng(vocab)
