@@ -258,29 +258,34 @@ __device__ __forceinline__ float least_logit(double edge, double offset) {
   return edge == kNone ? -__builtin_inff() : (float)(gap - 0x1p-20 * __builtin_fabs(gap) - 0x1p-40 * __builtin_fabs(offset));
 }
 
-// The keep-th candidate, bit by bit: first the greatest value that `keep` candidates reach, then of
+// The keep-th candidate, of which `floor` is known to be the value or less, and `end` an index past all, bit by bit: first
+// the greatest value that `keep` candidates reach, unless it is `floor` (rows of ties), then of
 // those that tie the least index up to which there are enough.
 template <typename Set>
-__device__ __forceinline__ Candidate find_edge(PickShared &s, int keep, const Set &set) {
-  unsigned long long k = 0;
+__device__ __forceinline__ Candidate find_edge(PickShared &s, int keep, const Set &set, double floor, int end) {
+  unsigned long long k = key_of(floor);
   int last = 0;
+  const int index_bits = 32 - __builtin_clz(end);
 #pragma unroll 1
-  for (int bit = 63 + 31; bit >= 0; --bit) {
-    const bool ties = bit < 31;
-    const unsigned long long key = ties ? k : k | 1ull << (bit - 31);
-    const int end = last | (ties ? 1 << bit : 0);
+  for (int bit = 64 + index_bits; bit >= 0; --bit) {
+    const bool first = bit == 64 + index_bits, ties = bit < index_bits;
+    const unsigned long long key = first ? k + 1 : ties ? k : k | 1ull << (bit - index_bits);
+    const int upto = last | (ties ? 1 << bit : 0);
     __syncthreads();
     if (threadIdx.x == 0) s.counted = 0;
     __syncthreads();
     int mine = 0;
-    set.above(kNone, [&](double v, int i) {
+    set.above(floor, [&](double v, int i) {
       const unsigned long long u = key_of(v);
-      mine += v > kNone && (ties ? u > key || (u == key && i < end) : u >= key);
+      mine += v > kNone && (ties ? u > key || (u == key && i < upto) : u >= key);
     });
     if (mine != 0) atomicAdd(&s.counted, mine);
     __syncthreads();
-    if (ties ? s.counted < keep : s.counted >= keep) {
-      if (ties) last = end; else k = key;
+    const int counted = s.counted;
+    if (first) {
+      if (counted < keep) bit = index_bits; else k = 0;
+    } else if (ties ? counted < keep : counted >= keep) {
+      if (ties) last = upto; else k = key;
     }
   }
   return Candidate{__builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k), last};
@@ -339,7 +344,7 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Can
     });
     __syncthreads();
     if (s.count <= kList || round > 0) break;
-    edge = find_edge(s, keep, set);
+    edge = find_edge(s, keep, set, edge.v, set.end());
     __syncthreads();
     if (tid == 0) s.count = 0;
     __syncthreads();
@@ -388,6 +393,7 @@ struct Chunks {
     }, with);
     return x;
   }
+  __device__ __forceinline__ int end() const { return a.n_beams * a.chunks; }
   template <typename Take>
   __device__ __forceinline__ void above(double edge, Take &&take) const {
     walk([&](int b, double offset) {
@@ -433,6 +439,7 @@ struct Tokens {
     // (it is one of them: not after the last)
     return Candidate{offset + (double)m, b * a.n_vocab + first + 3 * 128 + 7};
   }
+  __device__ __forceinline__ int end() const { return a.n_beams * a.n_vocab; }
   template <typename Take>
   __device__ __forceinline__ void above(double edge, Take &&take) const {
     if (offset == kNone) return;
