@@ -330,32 +330,60 @@ __device__ __forceinline__ void first_of_list(PickShared &s, int keep, int count
 
 // The `keep` first candidates, in order, to s.out_value and s.out_index; how many there are.  At least
 // `keep` reach the edge (or all do): those that do are listed, and a group of threads each counts the
-// ones before it.  Where they are more than the list holds, the edge is raised to the keep-th
-// candidate itself (eight of 4 x 32000 equal tokens: 72 us in all).  s.count is zero.
+// ones before it.  Where tokens are many, the edge is raised first: of the threads' first ones the keep-th is a
+// bound, and a thread has few behind it (28 of 14 x 543 tokens for 21 sequences, where the least chunk has few: 218 us
+// or more without, 27 with; 6 of 3 x 278 for 11, where nothing bounds them, 104 and 12; 1024 firsts at most).  Where
+// they are still more than the list holds, it is raised to the keep-th candidate itself (eight of 4 x 32000 equal
+// tokens: 81 us in all).  s.count is zero.
+constexpr int kShort = 256;
 template <typename Set>
 __device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Candidate edge) {
   const int tid = threadIdx.x;
-  for (int round = 0;; ++round) {
-    set.above(edge.v, [&](double v, int i) {
-      if (v > kNone && !before(edge.v, edge.i, v, i)) {
-        const int at = atomicAdd(&s.count, 1);
-        if (at < kList) s.value[at] = v, s.index[at] = i;
-      }
-    });
-    __syncthreads();
-    if (s.count <= kList || round > 0) break;
-    edge = find_edge(s, keep, set, edge.v, set.end());
+  const auto clear = [&]() {
     __syncthreads();
     if (tid == 0) s.count = 0;
     __syncthreads();
+  };
+  const auto add = [&](double v, int i) {
+    const int at = atomicAdd(&s.count, 1);
+    if (at < kList) s.value[at] = v, s.index[at] = i;
+  };
+  // (a step lists candidates, or threads' first ones; the list is put in order at one place, for less code)
+  bool firsts = Set::kRaise && edge.v == kNone, raised = firsts || !Set::kRaise;
+#pragma unroll 1
+  for (int most = raised ? kList : kShort;;) {
+    if (Set::kRaise && firsts) {
+      const Candidate x = set.best();
+      if (x.v > kNone && x.v >= edge.v) add(x.v, tid);
+    } else {
+      set.above(edge.v, [&](double v, int i) {
+        if (v > kNone && !before(edge.v, edge.i, v, i)) add(v, i);
+      });
+    }
+    __syncthreads();
+    const int count = min(s.count, kList);
+    if (!firsts && s.count > most) {
+      clear();
+      if (raised) {
+        edge = find_edge(s, keep, set, edge.v, set.end());
+        most = INT32_MAX;
+      } else {
+        firsts = raised = true;
+        most = kList;
+      }
+      continue;
+    }
+    first_of_list(s, keep, count);
+    if (!firsts) return min(count, keep);
+    edge = Candidate{count < keep ? edge.v : s.out_value[keep - 1], INT32_MAX};
+    firsts = false;
+    clear();
   }
-  const int count = min(s.count, kList);
-  first_of_list(s, keep, count);
-  return min(count, keep);
 }
 
 // Chunks, each of the value of its greatest token.  A beam's lie in `share` waves.
 struct Chunks {
+  static constexpr bool kRaise = false;     // (their edge is such a bound)
   const PickShared &s;
   const BeamArgs &a;
   const float *top;         // of the sequence
@@ -416,6 +444,7 @@ struct Chunks {
 // Tokens of the chosen chunks: a chunk is a group's, of 16 threads, with four times eight neighbours each.
 template <bool FP32>
 struct Tokens {
+  static constexpr bool kRaise = true;
   const BeamArgs &a;
   const void *row;          // of the chunk
   double offset;            // -infinity: no chunk
@@ -523,26 +552,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   if (tid == 0) s.count = 0;
   __syncthreads();
   const Tokens<FP32> tokens(s, a, row0, n_chunks);
-  if (n_chunks < a.n_keep) {
-    // (all chunks were chosen, and nothing bounds their tokens yet)
-    edge.v = kNone;
-    if (n_chunks * kBeamChunk > kList) {
-      // Of the threads' first tokens the n_keep-th does: n_keep reach it, in as many threads unless some tie, and
-      // a thread has 32.  Without it the edge is searched (32 of 16 x 500 tokens: 727 us, 19.7 with it).
-      const Candidate x = tokens.best();
-      if (x.v > kNone) {
-        const int at = atomicAdd(&s.count, 1);
-        s.value[at] = x.v;
-        s.index[at] = tid;
-      }
-      __syncthreads();
-      const int count = s.count;
-      first_of_list(s, a.n_keep, count);
-      if (count >= a.n_keep) edge.v = s.out_value[a.n_keep - 1];
-      if (tid == 0) s.count = 0;
-      __syncthreads();
-    }
-  }
+  if (n_chunks < a.n_keep) edge.v = kNone;      // (all chunks were chosen)
   const int n = pick(s, a.n_keep, tokens, edge);
   if (tid < a.n_keep) {
     const bool some = tid < n;

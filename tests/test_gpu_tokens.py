@@ -363,7 +363,8 @@ def test_rows_that_lie_gibibytes_apart():
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
 @pytest.mark.parametrize("seqs,beams,vocab,keep", [(2, 16, 500, 32), (1, 5, 512, 64), (3, 16, 150, 32), (1, 63, 300, 64), (2, 33, 512, 64),
-                                                   (1, 16, 1000, 64)])
+                                                   (1, 16, 1000, 64), (2, 7, 541, 14), (4, 16, 997, 32), (5, 14, 543, 28),
+                                                   (3, 1, 288, 2), (2, 3, 278, 6), (1, 6, 873, 12)])
 def test_choices_of_more_than_there_are_chunks(seqs, beams, vocab, keep, kind):
     rng = np.random.default_rng(beams + vocab)
     x = logits_of(rng, seqs, beams, vocab, kind)
