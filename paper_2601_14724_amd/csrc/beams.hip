@@ -133,10 +133,11 @@ __global__ __launch_bounds__(kRowThreads) void beam_rows(BeamArgs a) {
   float peak = -__builtin_inff();
   double sum = 0.0;
   float *const top = a.top + (int64_t)r * a.chunks;
-  // The greatest logit so far is `now`: older sums are scaled to it.
+  // The greatest logit so far is `now`: older sums are scaled to it.  (Times zero where there was none but
+  // -infinity: a NaN that came before stays one.)
   const auto raise = [&](float now) {
     if (now > peak) {
-      sum = peak == -__builtin_inff() ? 0.0 : sum * exp((double)peak - (double)now);
+      sum *= peak == -__builtin_inff() ? 0.0 : exp((double)peak - (double)now);
       peak = now;
     }
   };

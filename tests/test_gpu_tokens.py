@@ -332,6 +332,26 @@ def test_masked_tokens_and_rows_that_offer_nothing():
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [49999, 152064])
+def test_a_nan_before_a_wave_s_first_finite_step_is_not_lost(vocab, kind):
+    """Vocabularies of which a wave takes several steps.  Beams with NaN: all that a lane holds of the first
+    step, the first chunk, among masked tokens alone, with the sign set, in the last step of all.  None of them offers a token."""
+    rng = np.random.default_rng(vocab)
+    x = logits_of(rng, 2, 6, vocab, kind)
+    for s in range(2):
+        x[s, 0, :8] = np.nan
+        x[s, 1, 512 * s:512 * s + 512] = np.nan
+        x[s, 2, :4096] = -np.inf
+        x[s, 2, 77 + 1000 * s] = np.nan
+        x[s, 3, :8] = -np.float32(np.nan)
+        x[s, 3, 8:2048] = -np.inf
+        x[s, 4, vocab - 1 - 700 * s] = np.nan
+    score = np.float32([[0, 0, 0, 0, 0, -9]] * 2)
+    got = choose(x, score, 12, kind)
+    assert (got[1] == 5).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
 @pytest.mark.parametrize("allowed", [0, 5])
 def test_tokens_masked_by_the_lowest_value(kind, allowed):
     """Finite, so they are chosen where nothing else is left: whole rows of ties."""

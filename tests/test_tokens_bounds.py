@@ -153,6 +153,38 @@ def test_beam_select_stays_in_bounds_and_gives_the_definition(beams, seqs, n_bea
     check_choice(x.reshape(seqs, n_beams, vocab), score, done, keep, end, end_pad, got)
 
 
+def _nan_rows(n_beams, vocab, where):
+    """Logits of one sequence, whose first beam has a NaN in the first steps of a wave."""
+    x = (3 * np.random.default_rng(vocab).standard_normal((n_beams, vocab))).astype(np.float32)
+    if where == "eight":                     # all that a lane holds
+        x[0, :8] = np.nan
+    elif where == "chunk":
+        x[0, :512] = np.nan
+    elif where == "masked":                  # beside masked tokens alone
+        x[0, :2048] = -np.inf
+        x[0, 77] = np.nan
+    else:                                    # a NaN with the sign set, which orders below all
+        x[0, :8] = -np.float32(np.nan)
+        x[0, 8:512] = -np.inf
+    return x
+
+
+@pytest.mark.parametrize("where", ["eight", "chunk", "masked", "negative"])
+@pytest.mark.parametrize("vocab,per", [(1500, 2), (2300, 5), (4196, 8), (6000, 16)])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_a_nan_in_a_wave_s_first_steps_is_not_lost(beams, vocab, per, fp32, where):
+    """A beam one of whose logits is NaN offers nothing, whatever follows it."""
+    x = _nan_rows(2, vocab, where)
+    if not fp32:
+        x = pages.bf16_value(pages.bf16_bits(x)).astype(np.float32)
+    assert np.isnan(x[0]).any()
+    score = np.float32([[0, -5]])
+    out = run(beams, (1, 2, vocab, 4, fp32, vocab, 2, 2, False, per), x if fp32 else pages.bf16_bits(x), score)
+    got = cut(out, (np.float32, (1, 4)), (np.int32, (1, 4)), (np.int32, (1, 4)), (np.int32, (1, 4)))
+    assert got[1].tolist() == [[1] * 4]
+    check_choice(x[None], score, None, 4, 2, 2, got)
+
+
 @pytest.fixture(scope="module")
 def weights(tmp_path_factory):
     return compiled(tmp_path_factory, "weights", "-O1")
