@@ -640,9 +640,9 @@ int hermes_page_reorder(const hermes_page_pool *pool, const hermes_page_beams *b
  * the value
  *     (score[s][b] - ln sum_u exp(logits[s][b][u])) + logits[s][b][t]
  * in 64 bits, a beam that is done the one token pad_token, of value score[s][b].  (The
- * logarithm, through which beams are compared, is off by 1e-6 at most, where a row's
- * logits are a few values, and by about 1e-8 where they are many.)  Chosen are the greatest
- * values, a tie going to the lower beam and then to the lower token, and come in that order.  A
+ * logarithm, through which beams are compared, is off by 1e-6 at most in vocabularies of
+ * up to 2^20 tokens and by 1.5e-6 in larger ones, where a row's logits are a few values, and by
+ * about 1e-8 where they are many.)  Chosen are the greatest values, a tie going to the lower beam and then to the lower token, and come in that order.  A
  * token of logit -infinity is never chosen, nor is any of a beam whose score is not finite, or
  * one of whose logits is NaN or +infinity.  Where fewer than n_keep remain, parent and token are
  * -1, the score -infinity.

@@ -15,8 +15,11 @@
 // Beams meet through ln sum exp, and what is chosen are whole numbers, so it is found closer than in fp32:
 // differences to the greatest logit times log2 e in two fp32 steps (the second holds what log2 e as an
 // fp32 lacks), the hardware's exponential (1 ulp), eight of them added in fp32, all else in 64 bits.
-// Term by term that is 1e-6 at worst (an argument of 16 octaves and more has half an ulp of 2^-20), which
-// logits that differ average out: 1e-8.
+// Half an ulp of a difference of 8 to 16, and of its 11 to 23 octaves, are 2^-21 and 2^-20 ln 2; with the exponential's
+// ulp and three additions that is 1.4e-6 of a term.  Terms so far below their wave's greatest weigh little but where
+// a wave takes very many: 1e-6 of a row of 2^20 tokens at worst (7.2e-7 measured), 1.5e-6 of 2^30 (1.1e-6 of 2^27),
+// in rows of two values.  Logits that differ average it out: 1e-8.  (Differences and arguments in 64 bits are off by
+// 2e-7, and take 18.3 us for 17.5 of 16 x 8 beams.)
 //
 // Measured: 16 sequences of eight beams over 131072 tokens in bf16, 34 MB, 9.7 us (88 vector instructions
 // for 512 logits, its eight exponentials four issue slots each) and 9.5 for the choice; 32 of 16 in fp32,

@@ -428,6 +428,39 @@ def test_scores_of_steep_and_flat_rows():
                 assert abs(float(got[0][0, i]) - true) <= 2.0 ** -24 * abs(true) + DOUBT
 
 
+@pytest.mark.parametrize("n,parts,bound", [(2 ** 17, 64, DOUBT), (2 ** 20, 64, DOUBT), (2 ** 25, 64, 1.5e-6), (2 ** 25 + 77, 1, 1.5e-6)])
+def test_scores_of_two_values_whose_differences_round(n, parts, bound):
+    """ln sum exp of rows of a few peaks (the first token of every part) and one other value, so far below that its
+    difference to the peak and that one's octaves round, alike for all: nothing averages it out.  A term t below is off by half an ulp
+    of t, half an ulp of t log2 e times ln 2, an ulp of the exponential and three additions:
+      4 to 8      2^-22 + 2^-21 ln 2 + 2^-23 + 3 x 2^-24 = 8.7e-7
+      8 to 11     2^-21 + 2^-21 ln 2 + ..                = 1.11e-6
+      11.1 to 16  2^-21 + 2^-20 ln 2 + ..                = 1.44e-6
+      16 to 22.2  2^-20 + 2^-20 ln 2 + ..                = 1.92e-6
+    of its share, T e^-t / (1 + T e^-t) of a peak and T others.  A wave takes T tokens, and has a greatest of its own: T is
+    2^14 for 2^20 tokens (at 8 a share of 0.85: 9.4e-7; at 11.1 of 0.2) and 2^24 for the most that there may be (at 11.1 of
+    1: 1.44e-6; at 16 of 0.66: 1.26e-6).  The score is chosen so that the value is close to 0, and its rounding far below that."""
+    rng = np.random.default_rng(n)
+    rows, share = 4, -(-n // parts)
+    peak = rng.uniform(0, 6, 100000).astype(np.float32)
+    x = (peak - rng.uniform(4, 20, len(peak))).astype(np.float32)
+    far = x.astype(np.float64) - peak
+    octaves = ((x - peak).astype(np.float64) * 1.4426950408889634).astype(np.float32)
+    weight = share * np.exp(far) / (1 + share * np.exp(far))
+    off = (octaves * np.log(2) - far) * weight                # of the subtraction and the argument alone
+    pick = np.concatenate([np.argsort(off)[:rows // 2], np.argsort(-off)[:rows // 2]])
+    peak, x = peak[pick], x[pick]
+    logits = torch.from_numpy(x).to(DEV)[:, None].repeat(1, n)
+    logits[:, ::share] = torch.from_numpy(peak).to(DEV)[:, None]
+    p = peak.astype(np.float64)
+    lse = p + np.log(parts + (n - parts) * np.exp(x - p))
+    score = (lse - p).astype(np.float32)
+    got = H.beam_select(logits.view(rows, 1, n), torch.from_numpy(score).to(DEV).view(rows, 1), 1)
+    assert (got[2] == 0).all()
+    value = got[0].cpu().numpy()[:, 0].astype(np.float64)
+    assert (np.abs(value - ((score - lse) + p)) <= bound).all()
+
+
 def test_strides_that_are_no_rows_are_refused():
     x = torch.zeros(2, 3, 100, device=DEV)
     score = torch.zeros(2, 3, device=DEV)
