@@ -31,6 +31,7 @@ SCORE_CHUNK, SCORE_GUIDANCE = 0, 1
 PAGE_BF16, PAGE_FP4 = 0, 1
 PAGE_BAD_ID, PAGE_BAD_LENGTH, PAGE_BAD_ROWS, PAGE_BAD_PARENT, PAGE_NO_ROOM = 1, 2, 4, 8, 16
 BF16, FP32 = 0, 1
+_MOST = 0x7FFFFFFF   # (ctypes would keep the low half of a greater number)
 
 EXPORTED = ("hermes_workspace_bytes", "hermes_kv_init", "hermes_append_chunk",
             "hermes_append_chunk_at", "hermes_guidance_score", "hermes_compress",
@@ -670,6 +671,9 @@ class KVPages:
         self._fits(kv_len, torch.int32, shape[:-1], "kv_len")
         self._fits(parent, torch.int32, (n_seqs, n_beams), "parent")
         self._fits(room, torch.int32, shape[:-2] + (2,), "room")
+        n_groups = math.prod(shape[:-2])
+        if n_groups > _MOST or n_beams > _MOST or max_pages > _MOST or not 0 <= grow <= _MOST:
+            raise HermesError(EINVAL, "hermes_page_reorder")
         if tables_out is None:
             tables_out = torch.empty_like(tables)
         else:
@@ -678,7 +682,7 @@ class KVPages:
             kv_len_out = torch.empty_like(kv_len)
         else:
             self._fits(kv_len_out, torch.int32, shape[:-1], "kv_len_out")
-        s = PageBeamsStruct(math.prod(shape[:-2]), n_seqs, n_beams, max_pages, grow, parent.data_ptr(), room.data_ptr(),
+        s = PageBeamsStruct(n_groups, n_seqs, n_beams, max_pages, grow, parent.data_ptr(), room.data_ptr(),
                             tables.data_ptr(), kv_len.data_ptr(), tables_out.data_ptr(), kv_len_out.data_ptr())
         self._run(lib.hermes_page_reorder, "hermes_page_reorder", self._ref, ctypes.byref(s))
         return tables_out, kv_len_out
@@ -713,11 +717,14 @@ def beam_select(logits: torch.Tensor, score: torch.Tensor, keep: int, done: Opti
     _beams_of(score, torch.float32, (n_seqs, n_beams), index, "score")
     if done is not None:
         _beams_of(done, torch.int32, (n_seqs, n_beams), index, "done")
+    if (n_seqs > _MOST or n_beams > _MOST or n_vocab > _MOST or not 1 <= keep <= _MOST or not -1 <= end_token <= _MOST
+            or not 0 <= pad_token <= _MOST):
+        raise HermesError(EINVAL, "hermes_beam_select")
     cfg = BeamConfig(n_seqs, n_beams, n_vocab, keep, FP32 if logits.dtype is torch.float32 else BF16, end_token, pad_token)
     ref = ctypes.byref(cfg)
     nbytes = lib.hermes_beam_workspace_bytes(ref)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-    best, parent, token, ended = torch.empty((4, n_seqs, max(keep, 0)), dtype=torch.int32, device=logits.device).unbind(0)
+    best, parent, token, ended = torch.empty((4, n_seqs, keep), dtype=torch.int32, device=logits.device).unbind(0)
     best = best.view(torch.float32)
     _on(index, lib.hermes_beam_select, "hermes_beam_select", ref, logits.data_ptr(), stride, score.data_ptr(), _ptr(done),
         best.data_ptr(), parent.data_ptr(), token.data_ptr(), ended.data_ptr(), ws.data_ptr(), nbytes)
@@ -746,7 +753,7 @@ class PackedWeight:
         self.n_out, self.n_in = dense.shape
         self.device, self._index = dense.device, dense.get_device()
         w = WeightStruct(self.n_out, self.n_in, None)
-        nbytes = lib.hermes_weight_bytes(ctypes.byref(w))
+        nbytes = lib.hermes_weight_bytes(ctypes.byref(w)) if max(dense.shape) <= _MOST else 0
         if nbytes == 0:
             raise HermesError(EINVAL, "hermes_weight_bytes")
         self.data = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
@@ -764,6 +771,8 @@ class PackedWeight:
             raise ValueError(f"x: expected torch.bfloat16 [n_rows][{self.n_in}], got {getattr(x, 'dtype', None)} "
                              f"{tuple(getattr(x, 'shape', ()))}")
         n = x.shape[0]
+        if n > _MOST:
+            raise HermesError(EINVAL, "hermes_weight_product")
         shape = (n, self.n_out)
         self._on_device(x, "x")
         bp = ap = None

@@ -554,6 +554,24 @@ def test_reorder_refuses_other_tensors():
         pool.reorder(t, n, p, r, grow=-1)
 
 
+def test_numbers_past_32_bits_are_refused():
+    """(their low halves are those of good calls)"""
+    far = 2 ** 32
+    logits, score = torch.zeros(1, 2, 100, device=DEV), torch.zeros(1, 2, device=DEV)
+    pool = H.KVPages(2, 2, 64, 12, page_rows=16)
+    t, n, p, r = i32(np.zeros((2, 3, 4))), i32(np.zeros((2, 3))), i32(np.zeros((2, 3))), i32([[0, 3], [3, 3]])
+    w = H.PackedWeight(bf16(weight_bits(1, 8, 1)))
+    row = torch.zeros(1, 8, dtype=torch.bfloat16, device=DEV)
+    long = torch.empty(far + 16, dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: H.beam_select(logits, score, 2, end_token=far + 5), lambda: H.beam_select(logits, score, 2, end_token=-far + 5),
+                 lambda: H.beam_select(logits, score, 2, pad_token=far + 5), lambda: H.beam_select(logits, score, far + 2),
+                 lambda: H.beam_select(long.view(1, 1, -1), score[:, :1].contiguous(), 2),
+                 lambda: H.PackedWeight(long.view(-1, 1)), lambda: w.product(row.expand(far + 1, 8)),
+                 lambda: pool.reorder(t, n, p, r, grow=far + 1), lambda: pool.reorder(t, n, p, r, grow=1 - far)):
+        with pytest.raises(H.HermesError):
+            call()
+
+
 # --------------------------------------------------------------- as they are used
 class Model:
     """Two layers of one head group, products in 4 bits, and beams over their pages."""
