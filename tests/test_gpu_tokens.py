@@ -15,6 +15,7 @@ from oracle import pages_oracle as pages
 from oracle import tokens_oracle as orc
 from paper_2601_14724_amd import hermes as H
 from tests.test_tokens_bounds import DOUBT, beams_of, check_choice
+from tests.test_tokens_host import whole_numbers
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -127,6 +128,42 @@ def test_products_whose_inputs_are_shared_by_workgroups(m, n, k, out):
 @pytest.mark.parametrize("out", ["bf16", "fp32"])
 def test_products_whose_rows_are_shared_by_waves(m, n, k, out):
     check_product(m, n, k, out, bias=True, add=n < 10000, seed=n)
+
+
+# Every cut of the inputs and outputs that a product can have, with odd last tiles: up to 4, 8, 16, 32 and 64 rows;
+# one, two and four tiles of outputs a wave; inputs shared by one to eight waves, and by workgroups; rows shared by waves.
+WHOLE = [(1, 33, 5), (4, 5265, 5), (1, 33, 133), (4, 7985, 133), (1, 33, 515), (1, 14385, 1153), (1, 33, 903), (3, 2077, 5127),
+         (1, 67185, 1300), (1, 25585, 1300), (2, 25585, 2565), (1, 16465, 1300), (3, 16477, 1531), (5, 33, 515), (7, 1037, 600),
+         (5, 33, 903), (8, 2065, 1531), (5, 67185, 515), (5, 25585, 515), (7, 47985, 600), (5, 3185, 515), (7, 7997, 600),
+         (5, 3185, 903), (8, 5265, 1153), (5, 67185, 1300), (5, 25585, 1300), (8, 25585, 1531), (5, 5265, 1300), (7, 9757, 2700),
+         (5, 33, 5), (7, 9597, 300), (9, 33, 515), (16, 989, 600), (9, 33, 903), (13, 3025, 903), (9, 33, 5127), (9, 317, 20000),
+         (5, 47985, 5), (7, 47985, 300), (9, 3185, 515), (16, 3197, 600), (9, 3185, 903), (9, 3185, 2565), (9, 1025, 5127),
+         (9, 2045, 9005), (5, 67185, 5), (13, 131197, 300), (9, 5265, 515), (13, 5277, 600), (9, 5265, 903), (9, 14397, 2700),
+         (9, 2065, 5127), (16, 4945, 5127), (17, 33, 5), (24, 2045, 300), (17, 33, 515), (17, 977, 600), (17, 33, 903),
+         (17, 1025, 1531), (17, 33, 5127), (32, 305, 9005), (17, 47985, 5), (24, 47997, 903), (17, 3185, 515), (24, 3185, 600),
+         (17, 3185, 903), (32, 3185, 2003), (17, 1025, 5127), (24, 1025, 14336), (17, 67185, 5), (17, 131197, 515), (17, 5265, 515),
+         (17, 7997, 600), (17, 5265, 903), (24, 9597, 2003), (17, 2065, 5127), (24, 3025, 14336), (33, 33, 5), (33, 4945, 300),
+         (33, 33, 515), (64, 1037, 1531), (33, 33, 2565), (33, 977, 2700), (65, 16465, 5), (33, 47985, 1531), (33, 3185, 515),
+         (65, 3197, 1531), (33, 1025, 2565), (65, 2033, 5127), (33, 67185, 5), (130, 131185, 133), (33, 5265, 515), (50, 9745, 2565),
+         (33, 2065, 2565), (50, 7997, 2565), (9, 1000, 14336), (1, 300, 20000), (13, 4608, 8000), (16, 4608, 3584),
+         (64, 14336, 3584), (4, 1152, 18944)]
+
+
+@pytest.mark.parametrize("m,n,k", WHOLE)
+def test_products_of_whole_numbers_are_exact(m, n, k):
+    """Sums that fp32 holds whatever their order: equal bit for bit, in bf16 after the one rounding."""
+    x, w = whole_numbers(m, n, k, DEV)
+    packed = H.PackedWeight(w.to(torch.bfloat16))
+    rows = torch.full((m, -(-k // 8) * 8 + 8), float("nan"), dtype=torch.bfloat16, device=DEV)[:, :k]
+    rows.copy_(x)
+    want = torch.mm(x, w.T.contiguous())
+    assert torch.equal(packed.product(rows, dtype=torch.float32).double(), want)
+    bias = torch.arange(n, device=DEV) % 199 - 99.0
+    add = (torch.arange(m * n, device=DEV) % 251 - 125.0).view(m, n)
+    want += bias + add
+    extra = dict(bias=bias.to(torch.bfloat16), add=add.to(torch.bfloat16))
+    assert torch.equal(packed.product(rows, dtype=torch.float32, **extra).double(), want)
+    assert torch.equal(packed.product(rows, **extra), want.to(torch.bfloat16))
 
 
 @pytest.mark.parametrize("n", [50, 64])

@@ -193,6 +193,34 @@ def test_reference_product_of_one_row():
     assert out.tolist() == [[1.0, 78.0, 5.0]] and mag.tolist() == [[1.0, 78.0, 5.0]]
 
 
+def whole_numbers(m, n, k, device="cpu", seed=0):
+    """x [m][k], w [n][k] (fp64) of whole numbers, w as 4 bits hold them: a 6 in every 32 inputs makes their scale 1.
+    Sums of up to 2^18 terms stay below 2^24, so that fp32 holds every one of them, in any order and cut."""
+    g = torch.Generator(device=device).manual_seed(1000 * seed + m + n + k)
+    level = torch.tensor([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], dtype=torch.float64, device=device)
+    w = level[torch.randint(0, 11, (n, k), generator=g, device=device)]
+    w[:, ::32] = 6
+    w[::2, ::32] = -6
+    x = torch.randint(1, 8, (m, k), generator=g, device=device).double()
+    x[torch.rand((m, k), generator=g, device=device) < 0.5] *= -1
+    return x, w
+
+
+@pytest.mark.parametrize("m,n,k", [(9, 1000, 14336), (1, 300, 20000), (33, 33, 2565)])
+def test_whole_numbers_show_what_a_product_leaves_out(m, n, k):
+    """What exact tests of long products see: a piece of eight inputs, or the last few, left out or taken twice; and
+    parts of a sum that are rounded to bf16."""
+    x, w = whole_numbers(m, n, k)
+    bits = pages.bf16_bits(w[:40].numpy().astype(np.float32))
+    assert (orc.weight(bits) == w[:40].numpy()).all()
+    want = x @ w.T
+    assert 300 < want.abs().max() < 2 ** 24 and (want.float().double() == want).all()
+    for i in range(0, k, 8):
+        assert (x[:, i:i + 8] @ w[:, i:i + 8].T != 0).any()
+    halves = [(x[:, a:b] @ w[:, a:b].T).bfloat16().double() for a, b in ((0, k // 256 * 128), (k // 256 * 128, k))]
+    assert (halves[0] + halves[1] != want).any()
+
+
 def test_reference_choice_by_hand():
     logits = np.log(np.array([[0.5, 0.25, 0.25], [0.125, 0.125, 0.75]]))
     v, parent, token = orc.select(orc.values(logits, np.array([-1.0, -1.0])), 4)
