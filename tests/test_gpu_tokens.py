@@ -783,3 +783,58 @@ def test_calls_on_two_streams_at_once():
     for a, b in zip(want, got):
         for x, y in zip(a, b):
             assert all(torch.equal(p, q) for p, q in zip(x, y))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_in_turn_on_two_streams_that_overlap(captured):
+    """Products whose inputs workgroups share (through a workspace), choices and reorders, issued in turn on two streams
+    that both wait until all is issued; then as two graphs replayed at once, three times."""
+    n, k, m, steps = 1000, 14336, 64, 12
+    assert H.lib.hermes_weight_workspace_bytes(ctypes.byref(H.WeightStruct(n, k, None)), m) > 0
+    sides = []
+    for seed in (1, 2):
+        x, w = whole_numbers(m, n, k, DEV, seed)
+        rng = np.random.default_rng(seed)
+        n_pages, room, tables, kv_len, parent = beams_of(rng, 6, 3, 4, 5, 16, 40, False)
+        memory = torch.from_numpy(rng.integers(0, 255, (n_pages, 2 * pages.block_bytes(64, 16, "fp4"))).astype(np.uint8)).to(DEV)
+        sides.append(dict(w=H.PackedWeight(w.to(torch.bfloat16)), x=x.to(torch.bfloat16), want=torch.mm(x, w.T.contiguous()).float(),
+                          score=torch.zeros(8, 8, device=DEV), memory=memory,
+                          pool=H.KVPages(2, 2, 64, n_pages, page_rows=16, pages=memory.clone()),
+                          reorder=[i32(t) for t in (tables.reshape(2, 3, 4, 5), kv_len.reshape(2, 3, 4), parent, room.reshape(2, 3, 2))]))
+
+    def step(s):
+        logits = s["w"].product(s["x"], dtype=torch.float32)
+        return logits, *H.beam_select(logits.view(8, 8, n), s["score"], 16), *s["pool"].reorder(*s["reorder"]), s["pool"].pages.clone()
+    for s in sides:
+        s["alone"] = step(s)
+        assert torch.equal(s["alone"][0], s["want"])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    if captured:
+        graphs = []
+        for s, side, out in zip(sides, streams, got):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=side):
+                out.extend(step(s) for _ in range(steps))
+    for again in range(3 if captured else 1):
+        for s in sides:
+            s["pool"].pages.copy_(s["memory"])
+        torch.cuda.synchronize()
+        for side in streams:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)
+        if captured:
+            for side, graph in zip(streams, graphs):
+                with torch.cuda.stream(side):
+                    graph.replay()
+        else:
+            for _ in range(steps):
+                for s, side, out in zip(sides, streams, got):
+                    with torch.cuda.stream(side):
+                        out.append(step(s))
+        torch.cuda.synchronize()
+        for s, out in zip(sides, got):
+            assert len(out) == steps and s["pool"].faults() == 0
+            for results in out:
+                assert all(torch.equal(a, b) for a, b in zip(results, s["alone"]))
