@@ -255,8 +255,9 @@ __device__ __forceinline__ double value_of(unsigned long long key) {
 }
 
 // A set of candidates has end(), an index past all; count(value, upto), how many of this thread's are greater
-// than value or equal with an index below upto; best(), this thread's first one or one that comes shortly
-// after it; and above(edge, take), which calls take(value, index) of this thread's that may be edge or before it.
+// than value or equal with an index below upto; and above(edge, take), which calls take(value, index) of this
+// thread's that may be edge or before it.  Chunks have best(), this thread's first one; tokens greatest(), this
+// thread's greatest value.
 // Candidates of value -infinity do not count.
 
 // The least logit that an edge asks of a beam, or a little less: values are sums in 64 bits, and most logits
@@ -357,8 +358,10 @@ __device__ __forceinline__ int pick(PickShared &s, int keep, const Set &set, Can
 #pragma unroll 1
   for (int most = raised ? kList : kShort;;) {
     if (Set::kRaise && firsts) {
-      const Candidate x = set.best();
-      if (x.v > kNone && x.v >= edge.v) add(x.v, tid);
+      if constexpr (Set::kRaise) {
+        const double v = set.greatest();
+        if (v > kNone && v >= edge.v) add(v, tid);
+      }
     } else {
       set.above(edge.v, [&](double v, int i) {
         if (v > kNone && !before(edge.v, edge.i, v, i)) add(v, i);
@@ -466,16 +469,15 @@ struct Tokens {
 #pragma unroll
     for (int k = 0; k < 4; ++k) eight<FP32, false>(row, first + 128 * k, a.n_vocab, x[k]);
   }
-  __device__ __forceinline__ Candidate best() const {
-    if (offset == kNone) return Candidate{kNone, INT32_MAX};
-    if (done) return Candidate{threadIdx.x % kGroup == 0 ? offset : kNone, b * a.n_vocab + a.pad_token};
+  __device__ __forceinline__ double greatest() const {
+    if (offset == kNone) return kNone;
+    if (done) return threadIdx.x % kGroup == 0 ? offset : kNone;
     float m = x[0][0];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, x[k][j]);
-    // (it is one of them: not after the last)
-    return Candidate{offset + (double)m, b * a.n_vocab + first + 3 * 128 + 7};
+    return offset + (double)m;
   }
   __device__ __forceinline__ int end() const { return a.n_beams * a.n_vocab; }
   __device__ __forceinline__ int count(double value, int upto) const {
