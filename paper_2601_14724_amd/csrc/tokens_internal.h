@@ -24,7 +24,7 @@ struct WeightPackArgs {
 // 64 rows) waves / split x tiles tiles of outputs, `split` waves sharing the inputs of each.
 struct WeightPlan {
   int32_t row_quads;        // 1, 2, 4, 8 or 16
-  int32_t tiles;            // 1, 2 or 4
+  int32_t tiles;            // 1, 2 or 4 (2 at most with row_quads 1)
   int32_t log_split;        // split: 1, 2, 4 or 8 (4 at most with 64 rows)
   int32_t parts;            // workgroups that share the inputs; more than one: joined by a second launch
   int32_t common;           // four waves that share x in LDS (row_quads 4 and more, split and parts 1)

@@ -358,13 +358,11 @@ static void launch_product(const WeightProductArgs &a, hipStream_t s) {
 
 template <int RQ>
 static void launch_product(const WeightProductArgs &a, hipStream_t s) {
-  if (a.plan.tiles == 1) {
-    launch_product<RQ, 1>(a, s);
-  } else if (a.plan.tiles == 2) {
-    launch_product<RQ, 2>(a, s);
-  } else {
-    launch_product<RQ, 4>(a, s);
+  if (a.plan.tiles == 1) return launch_product<RQ, 1>(a, s);
+  if constexpr (RQ > 1) {       // (up to four rows have two tiles at most)
+    if (a.plan.tiles == 4) return launch_product<RQ, 4>(a, s);
   }
+  launch_product<RQ, 2>(a, s);
 }
 
 hipError_t launch_weight_product(const WeightProductArgs &a, hipStream_t s) {
