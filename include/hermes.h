@@ -613,7 +613,10 @@ int hermes_page_pack(hermes_ctx *ctx, int32_t layer, const hermes_page_pool *poo
  *  parent       device int32 [n_seqs][n_beams]; -1: the new beam is empty (length 0, no pages).
  *  room         device int32 [n_groups][2]: the first page of the group's room and its number
  *               of pages, 65536 at most.  Rooms of different groups hold no page in common.  A room
- *               that does not lie in the pool counts as empty (HERMES_PAGE_BAD_ID).
+ *               that does not lie in the pool counts as empty (HERMES_PAGE_BAD_ID).  A group's tables
+ *               name pages of its own room, or of none: a page of another group's room counts as
+ *               free there, so that this call may copy over it while it is read, and what it holds
+ *               from then on is undefined.
  *  tables, kv_len          device int32 [n_groups][n_beams][max_pages] and [n_groups][n_beams].
  *  tables_out, kv_len_out  the new ones, apart from the old.
  * The old tables must not be used again once rows have been appended by the new ones.

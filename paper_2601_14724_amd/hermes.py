@@ -660,7 +660,8 @@ class KVPages:
         """The (tables, kv_len) that beams go on with after a choice: beam j of sequence s continues
         beam parent[s][j] (int32 [n_seqs][n_beams]; -1: none), in every layer.  tables int32
         [n_seqs][n_beams][max_pages], or with layers before them; kv_len likewise without pages;
-        room int32 [.., n_seqs][2], first page and number of pages of the beams' own pages.
+        room int32 [.., n_seqs][2], first page and number of pages of the beams' own pages, which
+        the tables of no other group of beams name.
         Full pages are shared, a partly filled one that is not a beam's own is copied, and there
         is room for `grow` tokens more (hermes_page_reorder)."""
         if not isinstance(tables, torch.Tensor) or tables.dim() < 3:
