@@ -11,8 +11,8 @@
 //
 // Few bytes move (tables, and a page's live rows for every beam whose parent has another child), so small
 // calls are a chain: parents and lengths, the parents' tables, free pages, copies (one layer of four beams 3.4 us
-// without copies and 5.2 with, 1.8 of it an empty launch).  Large ones are bound by the copies, pieces of 1 to
-// 16 KiB at random places: 28 layers of 64 beams move 23 MB, 12.3 us, of which 4.3 are the chain.
+// without copies and 5.2 with, 1.8 of it an empty launch).  Large ones are bound by the copies, 1 to 16 KiB at random
+// places, which go piece by piece (see there): 28 layers of 64 beams move 23 MB, 12.3 us, of which 4.3 are the chain.
 #include "tokens_internal.h"
 
 namespace hermes {
@@ -159,7 +159,9 @@ __global__ __launch_bounds__(kThreads) void page_reorder(PageReorderArgs a) {
   }
   __syncthreads();
   // Copies: of every KV head's block the starts of K and of V with their scales (see PageBlock), a wave
-  // each, four loads at a time.
+  // each.  (Four pieces a lane are meant to be in flight.  As compiled, the conditional loads are waited for one by one
+  // and three of the four go through scratch memory, 80 bytes a lane: 15.9 MB written where pages and tables
+  // are 11.6, 28 layers of 64 beams.)
   const int jobs = s.copies * a.pool.Hkv * 2;
   for (int j = share * kWaves + wave; j < jobs; j += a.shares * kWaves) {
     const int b = s.copied[j / (2 * a.pool.Hkv)], part = j % 2, h = j / 2 % a.pool.Hkv;

@@ -11,8 +11,10 @@
 // v_mfma_f32_16x16x32_bf16 sums in fp32, so what is rounded is the sum alone.
 //
 // Measured (calls in one graph, weights not in the caches; an empty launch takes 1.8 us): 8 rows of 3584 on
-// 131072 outputs 46.6 us, 5.4 TB/s; one row on 4608 5.3, on 1152 x 896 2.9; 16 on 4608 6.7; 64 on 14336 15.6,
-// bound by L2, from which each workgroup reads all of x; 32 and 64 on 131072 52 and 64.
+// 131072 outputs 46.6 us, 5.4 TB/s; one row on 4608 5.3, on 1152 x 896 2.9; 16 on 4608 6.7; 64 on 14336 15.6;
+// 32 and 64 on 131072 52 and 64.  64 rows on 14336: reading x, 103 MB from L2, is 2.6 us of that (11.3 without any);
+// MFMAs are busy for 3.  The rest, by the code, is seven steps a wave that each wait for all of their loads, with one
+// more step asked for and, of 128 KiB of LDS a workgroup, one wave a SIMD.
 #include "tokens_internal.h"
 
 namespace hermes {
